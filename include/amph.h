@@ -328,6 +328,75 @@ amph_status amph_project_noalloc(const void* x_dev, int32_t x_rows_cap, const vo
                                  int32_t out, int32_t in, int32_t rows, int32_t dtype, int32_t use_tensor_core,
                                  float* y_dev, int32_t* status_dev, void* stream, char* err_msg, size_t err_len);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Operators for decoding many requests over one set of weights (no counterpart in the paper; they stand beside
+ * amph_project: stream-ordered, no context, device memory from the caller, the stream's device current).  Their status_dev (device
+ * int32, may be NULL) is set to an amph_status when a kernel meets a value that only the device can see (a page, sequence or
+ * adapter that does not exist, AMPH_ERR_INVALID_ARG; a bounded wait that gave up, AMPH_ERR_TIMEOUT) and is never cleared by them.
+ * Every other error is returned, with its message in amph_last_error(NULL), and nothing is launched.
+ * ------------------------------------------------------------------------------------------------------------------- */
+
+/* Low-rank adapters of many requests beside a shared projection.  Device arrays, 16-byte aligned, contiguous, of the
+ * projection's dtype: a [n_adapters][n_seg][rank][in], b [n_adapters][n_seg][out][rank]; scale: float [n_adapters], or NULL
+ * (1 for all).  rank: a multiple of 8, 8..AMPH_MAX_ADAPTER_RANK; adapters of a smaller rank are padded with zeros. */
+#define AMPH_MAX_ADAPTER_RANK 128
+typedef struct {
+  const void* a;
+  const void* b;
+  const float* scale;
+  int32_t n_adapters, rank;
+} amph_adapters;
+
+/* y[r][s*out + o] = sum_k x[r][k] w[s][o][k] + scale[i] sum_j (sum_k x[r][k] a[i][s][j][k]) b[i][s][o][j],  i = row_adapter[r]
+ * (device int32 [rows], any order; negative: the row has no adapter; >= n_adapters: the same, and status_dev is set).
+ * x, w, n_seg, out, in, rows (1..512), x_rows_cap, dtype and use_tensor_core as for amph_project.  y: [rows][n_seg*out] of
+ * y_dtype, 16-byte aligned (AMPH_DTYPE_F32, or AMPH_DTYPE_BF16 with bf16 weights: the sums, held in fp32, are rounded once).
+ * ws_dev: device scratch, 256-byte aligned, at least amph_project_adapters_bytes() bytes; nothing in it needs to be set and nothing
+ * is kept in it.  Calls that may overlap on the GPU need scratch of their own.  Make the first call on a device outside a stream capture. */
+amph_status amph_project_adapters_bytes(int32_t n_seg, int32_t out, int32_t rows, int32_t rank, size_t* ws_bytes);
+amph_status amph_project_adapters(const void* x_dev, int32_t x_rows_cap, const void* const* w, int32_t n_seg, int32_t out,
+                                  int32_t in, int32_t rows, int32_t dtype, int32_t use_tensor_core, const amph_adapters* adapters,
+                                  const int32_t* row_adapter, void* y_dev, int32_t y_dtype, void* ws_dev, size_t ws_bytes,
+                                  int32_t* status_dev, void* stream);
+
+/* One layer's paged cache: k_pages and v_pages [n_pages][n_kv_heads][page_size][head_dim] of dtype, device, 16-byte aligned.
+ * head_dim 64 or 128; page_size a power of two, at most 65536.  A page table (device int32 [n_seqs][table_stride]) names the
+ * pages of every sequence in order: position p of sequence s is slot p % page_size of page table[s][p / page_size].  Entries
+ * behind a sequence's last page are not read.  Sequences may share pages that no call writes. */
+typedef struct {
+  void* k_pages;
+  void* v_pages;
+  int32_t dtype, n_kv_heads, head_dim, page_size, n_pages;
+} amph_paged_cache;
+
+/* Rotary embedding (pairs (i, i + head_dim/2), angle pos * theta^(-2 i / head_dim)) of the rows' queries and keys, and the keys' and
+ * values' way into the pages.  Row r belongs to sequence row_seq[r] and sits at position row_pos[r] (device int32 [rows]); a
+ * row with row_seq[r] < 0 is skipped, nothing is written for it; one whose sequence, position or page does not exist is skipped and
+ * status_dev is set.  q, k, v: src_dtype [rows][n_heads or n_kv_heads][head_dim], rows q_stride / k_stride / v_stride
+ * ELEMENTS apart (slices of a projection's output), 16-byte aligned; AMPH_DTYPE_F32, or AMPH_DTYPE_BF16.  q_out: [rows][n_heads][head_dim] of the cache's dtype.  q = q_out = NULL
+ * with n_heads = 0: keys and values only.  Rows of one call must not name the same slot (which of them is kept is unspecified). */
+amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, int32_t src_dtype, int32_t n_heads, int32_t rows,
+                             const int32_t* row_seq, const int32_t* row_pos, const int32_t* table, int32_t n_seqs,
+                             int32_t table_stride, float theta, void* q_out, int32_t* status_dev, void* stream);
+
+/* Attention of one new token of every sequence over the sequence's pages:
+ *   out[s][h] = sum_p w_p V[p] / sum_p w_p,  w_p = exp(scale * q[s][h] . K[p]),  p = 0 .. lens[s] - 1, K and V of head h * n_kv_heads / n_heads
+ * lens: device int32 [n_seqs] (the new token included, so amph_paged_write comes first); 0: out[s] = 0.  A length outside
+ * 0 .. table_stride * page_size is clamped and status_dev is set; the keys of a page that does not exist count as absent, and status_dev is set.
+ * q, out: [n_seqs][n_heads][head_dim] of the cache's dtype, 16-byte aligned; out must not overlap q.  lse: float [n_seqs][n_heads], natural logarithm of
+ * sum_p w_p (-inf without keys), or NULL.  scale: 0 means 1 / sqrt(head_dim).  n_heads: a multiple of n_kv_heads, at most 1024;
+ * n_seqs at most AMPH_PAGED_MAX_SEQS.  ws_dev: device scratch of AMPH_PAGED_WS_BYTES, 256-byte aligned, for the parts of sequences that several
+ * blocks share.  Its first AMPH_PAGED_WS_COUNTERS bytes must be zero when the kernel starts, and every call leaves them zero: with
+ * ws_clean = 0 the call clears them itself (scratch with any contents), with ws_clean = 1 the caller vouches for them (cleared
+ * once, used by these calls alone).  Calls that may overlap on the GPU need scratch of their own.  Equal inputs give equal bits. */
+#define AMPH_PAGED_MAX_SEQS 4096
+#define AMPH_PAGED_WS_COUNTERS 4096u
+#define AMPH_PAGED_WS_BYTES (5u << 20)
+amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, int32_t n_heads, const int32_t* lens,
+                                 const int32_t* table, int32_t n_seqs, int32_t table_stride, float scale, void* out, float* lse,
+                                 void* ws_dev, size_t ws_bytes, int32_t ws_clean, int32_t* status_dev, void* stream);
+
 /* Per-category device time of the last amph_profile_begin / amph_profile_end pair: ms and launches are
  * HOST arrays of AMPH_PROF_CATEGORIES entries (either may be NULL).  While profiling, every kernel launch
  * (or pair: attention + merge) is bracketed by events, which serialises kernels that otherwise overlap. */

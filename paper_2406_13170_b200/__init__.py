@@ -1,7 +1,9 @@
 """B200 (sm_100a) Amphista speculative-decoding step: ctypes binding of libamph.so."""
 from .binding import (  # noqa: F401
+    Adapters,
     AmphError,
     Amphista,
+    PagedCache,
     amph_config,
     amph_tensor,
     amph_tree,
@@ -9,6 +11,9 @@ from .binding import (  # noqa: F401
     library_path,
     make_config,
     make_tree,
+    paged_attention,
+    paged_write,
     project,
+    project_adapters,
     project_noalloc,
 )

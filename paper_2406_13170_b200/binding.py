@@ -27,7 +27,12 @@ STATUS = {0: "AMPH_OK", 1: "AMPH_ERR_INVALID_ARG", 2: "AMPH_ERR_SHAPE", 3: "AMPH
 EXPORTS = ["amph_workspace_bytes", "amph_init", "amph_load_weights", "amph_prefill", "amph_prefill_seq", "amph_get_state_seq", "amph_draft",
            "amph_verify_tree", "amph_accept", "amph_step", "amph_get_tensor", "amph_set_tensor",
            "amph_get_state", "amph_set_state", "amph_selftest_wait_timeout", "amph_selftest_context_timeout", "amph_profile_begin", "amph_profile_end", "amph_profile_breakdown", "amph_project", "amph_project_noalloc",
+           "amph_project_adapters_bytes", "amph_project_adapters", "amph_paged_write", "amph_paged_attention",
            "amph_reset", "amph_destroy", "amph_last_error"]
+AMPH_MAX_ADAPTER_RANK = 128
+AMPH_PAGED_MAX_SEQS = 4096
+AMPH_PAGED_WS_COUNTERS = 4096
+AMPH_PAGED_WS_BYTES = 5 << 20
 
 
 class amph_config(C.Structure):
@@ -48,6 +53,15 @@ class amph_tree(C.Structure):
 class amph_tensor(C.Structure):
     _fields_ = [("name", C.c_char_p), ("dev_ptr", C.c_void_p), ("dtype", C.c_int32),
                 ("ndim", C.c_int32), ("shape", C.c_int64 * 4)]
+
+
+class amph_adapters(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p), ("n_adapters", C.c_int32), ("rank", C.c_int32)]
+
+
+class amph_paged_cache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("dtype", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32)]
 
 
 class AmphError(RuntimeError):
@@ -99,6 +113,14 @@ def lib() -> C.CDLL:
                                    C.c_int32, C.c_int32, vp, vp, C.c_size_t, vp]
         L.amph_project_noalloc.argtypes = [vp, C.c_int32, C.POINTER(vp), C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                            C.c_int32, C.c_int32, vp, vp, vp, C.c_char_p, C.c_size_t]
+        i32, i64 = C.c_int32, C.c_int64
+        L.amph_project_adapters_bytes.argtypes = [i32, i32, i32, i32, C.POINTER(C.c_size_t)]
+        L.amph_project_adapters.argtypes = [vp, i32, C.POINTER(vp), i32, i32, i32, i32, i32, i32, C.POINTER(amph_adapters), vp, vp, i32,
+                                            vp, C.c_size_t, vp, vp]
+        L.amph_paged_write.argtypes = [C.POINTER(amph_paged_cache), vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, vp, vp, i32, i32,
+                                       C.c_float, vp, vp, vp]
+        L.amph_paged_attention.argtypes = [C.POINTER(amph_paged_cache), vp, i32, vp, vp, i32, i32, C.c_float, vp, vp, vp, C.c_size_t,
+                                           i32, vp, vp]
         L.amph_reset.argtypes = [vp]
         L.amph_destroy.argtypes = [vp]
         L.amph_destroy.restype = None
@@ -386,3 +408,231 @@ def project_noalloc(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use_
                                     msg, len(msg))
     if rc != 0:
         raise AmphError(rc, msg.value.decode())
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Operators for decoding many requests over one set of weights.  They run on torch's current stream of the tensors' device, never
+# synchronise, and return tensors whose contents are there in stream order.
+# ---------------------------------------------------------------------------------------------------------------------
+_DTYPES = {torch.float32: AMPH_DTYPE_F32, torch.bfloat16: AMPH_DTYPE_BF16}
+
+
+def _refuse(status: int, message: str):
+    raise AmphError(status, message)
+
+
+def _want(t: torch.Tensor, name: str, device: torch.device, dtype, shape=None) -> torch.Tensor:
+    """A contiguous tensor of this type and shape on this device, or an AmphError."""
+    if t.dtype is not dtype:
+        _refuse(1, f"{name} must be {dtype} (got {t.dtype})")
+    if t.device != device:
+        _refuse(1, f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        _refuse(1, f"{name} must be contiguous")
+    if shape is not None and t.shape != shape:
+        _refuse(2, f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+    return t
+
+
+def _call(L, fn, index: int, args) -> None:
+    """fn(*args, current stream) with device `index` current."""
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if rc != 0:
+        raise AmphError(rc, L.amph_last_error(None).decode())
+
+
+class Adapters:
+    """Low-rank adapters of a projection with n_seg weight matrices (amph_adapters).
+
+    a [n_adapters, n_seg, rank, in], b [n_adapters, n_seg, out, rank] (fp32 or bf16, the projection's type), scale fp32
+    [n_adapters] or None.  rank: a multiple of 8, at most 128; smaller ranks are padded with zeros.  The tensors are borrowed.
+    """
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None):
+        if a.dim() != 4 or b.dim() != 4 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[1] or a.shape[2] != b.shape[3]:
+            _refuse(2, f"adapters: a {tuple(a.shape)} and b {tuple(b.shape)} do not fit together")
+        if a.dtype not in _DTYPES:
+            _refuse(2, f"adapters must be float32 or bfloat16 (got {a.dtype})")
+        if not a.is_cuda:
+            _refuse(7, "adapters must be on a CUDA device")
+        _want(a, "a", a.device, a.dtype)
+        _want(b, "b", a.device, a.dtype)
+        self.n, self.n_seg, self.rank, self.in_ = a.shape
+        self.out, self.dtype, self.device = b.shape[2], a.dtype, a.device
+        if self.n < 1:
+            _refuse(2, "no adapters")
+        if scale is not None:
+            _want(scale, "scale", a.device, torch.float32, (self.n,))
+        self.tensors = (a, b, scale)
+        self.c = amph_adapters(a.data_ptr(), b.data_ptr(), None if scale is None else scale.data_ptr(), self.n, self.rank)
+
+
+def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use_tensor_core: bool, adapters: Adapters,
+                     row_adapter: torch.Tensor, y: Optional[torch.Tensor] = None, y_dtype: Optional[torch.dtype] = None,
+                     status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """amph_project_adapters: y[r] = x[r] . W^T + scale (x[r] . a^T) . b^T with the adapter row_adapter[r] (int32 [rows], < 0: none).
+
+    x, ws, rows, use_tensor_core as for `project`; y [rows, n_seg * out] of y_dtype (default: x's type)."""
+    L = lib()
+    n_seg, dev, dt = len(ws), x.device, x.dtype
+    if dt not in _DTYPES or x.dim() != 2 or n_seg < 1:
+        _refuse(2, f"x must be a float32 or bfloat16 matrix (got {dt}, {tuple(x.shape)}), with at least one weight matrix")
+    if not x.is_cuda:
+        _refuse(7, "x must be on a CUDA device")
+    _want(x, "x", dev, dt)
+    out, in_ = ws[0].shape
+    for w in ws:
+        _want(w, "w", dev, dt, (out, in_))
+    if x.shape[1] != in_ or adapters.in_ != in_ or adapters.out != out or adapters.n_seg != n_seg:
+        _refuse(2, f"x {tuple(x.shape)}, {n_seg} weights {(out, in_)} and adapters {tuple(adapters.tensors[0].shape)} / "
+                   f"{tuple(adapters.tensors[1].shape)} do not fit together")
+    if adapters.dtype is not dt or adapters.device != dev:
+        _refuse(1, f"the adapters are {adapters.dtype} on {adapters.device}, x is {dt} on {dev}")
+    _want(row_adapter, "row_adapter", dev, torch.int32, (rows,))
+    if y is None:
+        y = torch.empty(rows, n_seg * out, dtype=y_dtype or dt, device=dev)
+    else:
+        if y_dtype is not None and y.dtype is not y_dtype:
+            _refuse(1, f"y is {y.dtype}, not {y_dtype}")
+        _want(y, "y", dev, y.dtype, (rows, n_seg * out))
+    if y.dtype not in _DTYPES:
+        _refuse(2, f"y must be float32 or bfloat16 (got {y.dtype})")
+    if status is not None:
+        _want(status, "status", dev, torch.int32)
+    need = C.c_size_t()
+    rc = L.amph_project_adapters_bytes(n_seg, out, rows, adapters.rank, C.byref(need))
+    if rc != 0:
+        raise AmphError(rc, L.amph_last_error(None).decode())
+    scratch = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    arr = (C.c_void_p * n_seg)(*[w.data_ptr() for w in ws])
+    _call(L, L.amph_project_adapters, dev.index,
+          (x.data_ptr(), x.shape[0], arr, n_seg, out, in_, rows, _DTYPES[dt], int(use_tensor_core), C.byref(adapters.c),
+           row_adapter.data_ptr(), y.data_ptr(), _DTYPES[y.dtype], scratch.data_ptr(), need.value,
+           None if status is None else status.data_ptr()))
+    return y
+
+
+class PagedCache:
+    """One layer's keys and values in pages (amph_paged_cache): k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim], fp32
+    or bf16, borrowed.  A page table is int32 [n_seqs, width]: position p of sequence s lies in page table[s, p // page_size]."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
+        if k_pages.dim() != 4 or k_pages.dtype not in _DTYPES:
+            _refuse(2, f"k_pages must be [n_pages, n_kv_heads, page_size, head_dim], float32 or bfloat16 (got {tuple(k_pages.shape)}, {k_pages.dtype})")
+        if not k_pages.is_cuda:
+            _refuse(7, "pages must be on a CUDA device")
+        self.device, self.dtype = k_pages.device, k_pages.dtype
+        _want(k_pages, "k_pages", self.device, self.dtype)
+        _want(v_pages, "v_pages", self.device, self.dtype, k_pages.shape)
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
+        self.c = amph_paged_cache(k_pages.data_ptr(), v_pages.data_ptr(), _DTYPES[self.dtype], self.n_kv_heads, self.head_dim,
+                                  self.page_size, self.n_pages)
+        self.ref = C.byref(self.c)
+
+    def _table(self, table: torch.Tensor) -> torch.Tensor:
+        if table.dim() != 2:
+            _refuse(2, f"table must be [n_seqs, width] (got {tuple(table.shape)})")
+        return _want(table, "table", self.device, torch.int32)
+
+
+def _rows_of(t: torch.Tensor, name: str, cache: PagedCache, rows: int, heads: int, dtype) -> int:
+    """Checks [rows, heads * head_dim] or [rows, heads, head_dim] whose rows are contiguous; returns the row stride in elements."""
+    if t.dtype is not dtype or t.device != cache.device:
+        _refuse(1, f"{name} must be {dtype} on {cache.device} (got {t.dtype} on {t.device})")
+    dh = cache.head_dim
+    if t.dim() == 2:
+        fits = t.shape[0] == rows and t.shape[1] == heads * dh and t.stride(1) == 1
+    else:
+        fits = t.dim() == 3 and t.shape == (rows, heads, dh) and t.stride(2) == 1 and (t.stride(1) == dh or heads == 1)
+    if not fits:
+        _refuse(2, f"{name} must be {rows} rows of {heads} heads of {dh}, each row contiguous (got {tuple(t.shape)}, strides {t.stride()})")
+    return t.stride(0) if rows > 1 else heads * dh
+
+
+def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, row_seq: torch.Tensor,
+                row_pos: torch.Tensor, table: torch.Tensor, theta: float = 10000.0, q_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """amph_paged_write: rotates q and k of every row by its position, puts k and v into the pages, returns q.
+
+    q [rows, n_heads * head_dim] (or None), k, v [rows, n_kv_heads * head_dim], fp32 or bf16 (one type), each row contiguous (slices
+    of a projection's output); row_seq, row_pos int32 [rows], row_seq < 0: the row is skipped (its place in a new q_out is not set)."""
+    L = lib()
+    dev, rows = cache.device, k.shape[0]
+    if k.dtype not in _DTYPES:
+        _refuse(2, f"k must be float32 or bfloat16 (got {k.dtype})")
+    ks = _rows_of(k, "k", cache, rows, cache.n_kv_heads, k.dtype)
+    vs = _rows_of(v, "v", cache, rows, cache.n_kv_heads, k.dtype)
+    heads = qs = 0
+    if q is not None:
+        heads = (q.shape[1] * q.shape[2] if q.dim() == 3 else q.shape[-1]) // cache.head_dim
+        qs = _rows_of(q, "q", cache, rows, heads, k.dtype)
+        if q_out is None:
+            q_out = torch.empty(rows, heads, cache.head_dim, dtype=cache.dtype, device=dev)
+        else:
+            _want(q_out, "q_out", dev, cache.dtype, (rows, heads, cache.head_dim))
+    elif q_out is not None:
+        _refuse(1, "q_out without q")
+    _want(row_seq, "row_seq", dev, torch.int32, (rows,))
+    _want(row_pos, "row_pos", dev, torch.int32, (rows,))
+    cache._table(table)
+    if status is not None:
+        _want(status, "status", dev, torch.int32)
+    _call(L, L.amph_paged_write, dev.index,
+          (cache.ref, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[k.dtype], heads, rows,
+           row_seq.data_ptr(), row_pos.data_ptr(), table.data_ptr(), table.shape[0], table.shape[1], theta,
+           None if q is None else q_out.data_ptr(), None if status is None else status.data_ptr()))
+    return q_out
+
+
+_attention_scratch: Dict[tuple, torch.Tensor] = {}      # (device, stream) -> scratch whose counters are zero between calls
+
+
+def paged_attention(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, scale: float = 0.0,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """amph_paged_attention: one new token of every sequence, q [n_seqs, n_heads, head_dim], against positions 0 .. lens - 1 of its
+    pages.  lens int32 [n_seqs]; lse fp32 [n_seqs, n_heads] receives the logarithm of the softmax's sums; scale 0: 1 / sqrt(head_dim).
+
+    The scratch belongs to the stream that the call runs on: one piece per stream, kept; a call that is captured into a
+    graph has its own, from the graph's memory."""
+    dev = cache.device
+    index = dev.index
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return paged_attention(cache, q, table, lens, scale, out, lse, status)
+    L = lib()
+    if q.dim() != 3:
+        _refuse(2, f"q must be [n_seqs, n_heads, head_dim] (got {tuple(q.shape)})")
+    n, heads, dh = q.shape
+    _want(q, "q", dev, cache.dtype, (n, heads, cache.head_dim))
+    cache._table(table)
+    if table.shape[0] != n:
+        _refuse(2, f"table has {table.shape[0]} rows for {n} sequences")
+    _want(lens, "lens", dev, torch.int32, (n,))
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _want(out, "out", dev, cache.dtype, q.shape)
+    if lse is not None:
+        _want(lse, "lse", dev, torch.float32, (n, heads))
+    if status is not None:
+        _want(status, "status", dev, torch.int32)
+    clean = 0
+    if torch.cuda.is_current_stream_capturing():
+        scratch = torch.empty(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=dev)
+    else:
+        key = (index, torch._C._cuda_getCurrentRawStream(index))
+        scratch = _attention_scratch.get(key)
+        clean = 1
+        if scratch is None:
+            scratch = _attention_scratch[key] = torch.zeros(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=dev)
+    _call(L, L.amph_paged_attention, index,
+          (cache.ref, q.data_ptr(), heads, lens.data_ptr(), table.data_ptr(), n, table.shape[1], scale, out.data_ptr(),
+           None if lse is None else lse.data_ptr(), scratch.data_ptr(), AMPH_PAGED_WS_BYTES, clean,
+           None if status is None else status.data_ptr()))
+    return out

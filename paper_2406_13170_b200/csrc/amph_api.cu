@@ -165,6 +165,21 @@ amph_status fail(amph_ctx* ctx, amph_status code, const char* fmt, ...) {
   return code;
 }
 
+}  // namespace
+
+namespace amph {
+amph_status api_fail(amph_status code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(nullptr, code, "%s", buf);
+}
+}  // namespace amph
+
+namespace {
+
 // Brackets the launches issued during its lifetime with a pair of events (only while profiling).
 struct ProfScope {
   amph_ctx* ctx;

@@ -135,6 +135,9 @@ __device__ __forceinline__ float row_scale(const RowScale& rs, int row) {
 }
 #endif
 
+// The status of a call that has no context, and its message for amph_last_error(NULL).
+amph_status api_fail(amph_status code, const char* fmt, ...);
+
 // ---- launchers (one per kernel family); dtype = AMPH_DTYPE_* of weights / activations / cache
 // Rows of a pass in G groups of rpg: where their positions come from and where the row / rotary tables go (group 0's copy, the
 // next group's `stride` bytes further on).

@@ -1,0 +1,603 @@
+// Paged key / value caches: amph_paged_write (rotary embedding, keys and values into their pages) and amph_paged_attention
+// (one new token of every sequence against its pages).
+#include <math.h>
+#include <string.h>
+
+#include "amph_internal.cuh"
+
+namespace amph {
+namespace {
+
+typedef __nv_bfloat16 bf16;
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// amph_paged_write
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int kWriteThreads = 256;
+
+struct WriteParams {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  void *q_out, *k_pages, *v_pages;
+  const int *row_seq, *row_pos, *table;
+  int* status;
+  int n_seqs, table_stride, n_heads, n_kv, dh, page_shift, n_pages;
+  u64 turn[64];            // theta^(-2 i / dh) / (2 pi) as a fraction of 2^64: the share of a turn per position
+};
+
+// cos and sin of the angle whose share of a full turn is phase / 2^64.  The product position * turn wraps at whole turns, so the
+// phase of any position is exact to 2^-64 * position; what fp32 rounds is an angle of at most pi / 4.
+__device__ __forceinline__ float2 cos_sin_of_phase(u64 phase) {
+  const uint32_t top = (uint32_t)(phase >> 32);
+  const uint32_t quadrant = (top + 0x20000000u) >> 30;
+  const int rest = (int)(top - (quadrant << 30));                    // [-2^29, 2^29): an eighth of a turn either way
+  float s, c;
+  sincospif((float)rest * 4.656612873077393e-10f, &s, &c);           // 2^-31: in units of half a turn
+  if (quadrant & 1) { const float x = s; s = c; c = -x; }
+  if (quadrant & 2) { s = -s; c = -c; }
+  return make_float2(c, s);
+}
+
+// Grid (row, part of the row's heads); a thread takes eight rotation pairs of one head at a time (eight values twice for v).
+// Bound: HBM for many rows, latency for few: the rows' loads do not depend on the table's, and several parts share a row.
+template <typename TS, typename TD>
+__global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid_constant__ WriteParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ float2 cs[64];
+  const int row = blockIdx.x, half = p.dh >> 1;
+  const int seq = p.row_seq[row], pos = p.row_pos[row];
+  if (seq < 0) return;
+  bool ok = seq < p.n_seqs && pos >= 0 && (pos >> p.page_shift) < p.table_stride;
+  int page = 0;
+  if (ok) {
+    page = p.table[(int64_t)seq * p.table_stride + (pos >> p.page_shift)];
+    ok = page >= 0 && page < p.n_pages;
+  }
+  if (!ok) {
+    if (p.status != nullptr && threadIdx.x == 0) *p.status = AMPH_ERR_INVALID_ARG;
+    return;
+  }
+  if (threadIdx.x < half) cs[threadIdx.x] = cos_sin_of_phase((u64)pos * p.turn[threadIdx.x]);
+  __syncthreads();
+  const int per_head = half >> 3;
+  const int items = (p.n_heads + 2 * p.n_kv) * per_head;
+  const int64_t slot = pos & ((1 << p.page_shift) - 1);
+  for (int it = blockIdx.y * kWriteThreads + threadIdx.x; it < items; it += gridDim.y * kWriteThreads) {
+    const int head = it / per_head, i = (it - head * per_head) * 8;
+    const TS* src;
+    TD* dst;
+    if (head < p.n_heads) {
+      src = (const TS*)p.q + row * p.q_stride + head * p.dh;
+      dst = (TD*)p.q_out + ((int64_t)row * p.n_heads + head) * p.dh;
+    } else {
+      const int h = head - p.n_heads, is_v = h >= p.n_kv, hk = is_v ? h - p.n_kv : h;
+      src = is_v ? (const TS*)p.v + row * p.v_stride : (const TS*)p.k + row * p.k_stride;
+      src += hk * p.dh;
+      dst = (TD*)(is_v ? p.v_pages : p.k_pages) + ((((int64_t)page * p.n_kv + hk) << p.page_shift) + slot) * p.dh;
+    }
+    float a[8], b[8];
+    load8(src + i, a);
+    load8(src + half + i, b);
+    if (head < p.n_heads + p.n_kv) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float2 t = cs[i + j];
+        const float lo = a[j] * t.x - b[j] * t.y;
+        b[j] = b[j] * t.x + a[j] * t.y;
+        a[j] = lo;
+      }
+    }
+    store8(dst + i, a);
+    store8(dst + half + i, b);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// amph_paged_attention
+//
+// The work is a line of units of kUnit keys: sequence by sequence, in a sequence item by item (a key / value head and up to kHeads of
+// the query heads that share it), in an item unit by unit.  The grid is as many blocks as the device runs at a time, and
+// block c takes units [total * c / n, total * (c + 1) / n): every length mix is spread evenly, and the host needs no length.  An item
+// inside one block is finished there.  Of an item cut over blocks each leaves its part (running maximum, sum, weighted values)
+// in scratch, and the block that arrives last adds the parts in the order of the blocks: no block waits, and the
+// bits do not depend on who is last.  Statistics and sums are fp32.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int kUnit = 64;                // keys: 16 for each warp
+constexpr int kAttWarps = 4;
+constexpr int kAttThreads = kAttWarps * 32;
+constexpr int kHeads = 8;                // query heads of an item
+constexpr int kMaxBlocks = 592;
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct AttendParams {
+  const void *q, *k, *v;
+  const int *lens, *table;
+  void* out;
+  float* lse;
+  int* counters;           // [kMaxBlocks]: parts that arrived of the item that begins in block c and goes on behind it
+  float* parts;            // [kMaxBlocks][2][part_floats]: block c's part of an item that began before it | begins in it
+  int* status;
+  int part_floats;
+  int n_seqs, table_stride, n_heads, n_kv, group, head_blocks, page_shift, n_pages;
+  int cap;                 // positions a table row has room for
+  float scale_log2;
+};
+
+template <int DH>
+struct __align__(16) MergeSmem {
+  float o[kAttWarps][kHeads][DH];
+  float m[kAttWarps][kHeads], l[kAttWarps][kHeads];
+};
+
+__device__ __forceinline__ int clamped_len(const AttendParams& p, int s) {
+  const int n = p.lens[s];
+  return n < 0 ? 0 : (n > p.cap ? p.cap : n);
+}
+
+// exp2(x - m) of a running maximum m that may still be -inf (nothing seen)
+__device__ __forceinline__ float weight(float x, float m) { return exp2f(x - (m == -INFINITY ? 0.f : m)); }
+
+// First key of the 16 at `key` (page_size >= 16: they share a page); a page that does not exist is reported and counts as absent.
+__device__ __forceinline__ int page_of(const AttendParams& p, int seq, int key) {
+  const int page = p.table[(int64_t)seq * p.table_stride + (key >> p.page_shift)];
+  if (page >= 0 && page < p.n_pages) return page;
+  if (p.status != nullptr) *p.status = AMPH_ERR_INVALID_ARG;
+  return -1;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+  if constexpr (sizeof(T) == 4 && N == 4) {
+    const float4 a = *reinterpret_cast<const float4*>(p);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  } else if constexpr (sizeof(T) == 4) {
+    const float2 a = *reinterpret_cast<const float2*>(p);
+    v[0] = a.x; v[1] = a.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const uint32_t u = *reinterpret_cast<const uint32_t*>(p + i);
+      v[i] = __uint_as_float(u << 16);
+      v[i + 1] = __uint_as_float(u & 0xffff0000u);
+    }
+  }
+}
+
+// Keys [k0, k1) of one item by CUDA cores: scores with eight lanes per key, weighted values with every lane on its own columns.
+template <typename T, int DH>
+struct PlainItem {
+  struct Smem {
+    float q[kHeads][DH];
+    float s[kAttWarps][kHeads][16];
+    float alpha[kAttWarps][kHeads];
+  };
+  static __device__ void run(const AttendParams& p, Smem& sm, MergeSmem<DH>& out, int seq, int kv, int head0, int heads, int k0, int k1) {
+    constexpr int C = DH / 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int i = tid; i < heads * DH; i += kAttThreads)
+      sm.q[i / DH][i % DH] = to_f(((const T*)p.q)[((int64_t)seq * p.n_heads + head0) * DH + i]);
+    __syncthreads();
+    const T* kp = (const T*)p.k;
+    const T* vp = (const T*)p.v;
+    const int page_mask = (1 << p.page_shift) - 1;
+    float o[kHeads][C];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[h][c] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    const int my_head = lane >> 2;
+    for (int key0 = k0 + warp * 16; key0 < k1; key0 += kUnit) {
+      for (int i = 0; i < 4; ++i) {
+        const int j = i * 4 + (lane >> 3), key = key0 + j;
+        int page = -1;
+        if (key < k1) page = page_of(p, seq, key);
+        float kf[C][4];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if (page >= 0)
+            load_n<T, 4>(kp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + c * 32 + (lane & 7) * 4, kf[c]);
+          else
+            kf[c][0] = kf[c][1] = kf[c][2] = kf[c][3] = 0.f;
+        }
+        for (int h = 0; h < heads; ++h) {
+          float acc = 0.f;
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const float4 qv = *reinterpret_cast<const float4*>(&sm.q[h][c * 32 + (lane & 7) * 4]);
+            acc += kf[c][0] * qv.x; acc += kf[c][1] * qv.y; acc += kf[c][2] * qv.z; acc += kf[c][3] * qv.w;
+          }
+          acc += __shfl_xor_sync(~0u, acc, 1);
+          acc += __shfl_xor_sync(~0u, acc, 2);
+          acc += __shfl_xor_sync(~0u, acc, 4);
+          if ((lane & 7) == 0) sm.s[warp][h][j] = page >= 0 ? acc * p.scale_log2 : -INFINITY;
+        }
+      }
+      __syncwarp();
+      if (my_head < heads) {
+        float4 s = *reinterpret_cast<float4*>(&sm.s[warp][my_head][(lane & 3) * 4]);
+        float mx = fmaxf(fmaxf(s.x, s.y), fmaxf(s.z, s.w));
+        const unsigned quad = 0xfu << (lane & ~3);
+        mx = fmaxf(mx, __shfl_xor_sync(quad, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(quad, mx, 2));
+        mx = fmaxf(mx, m_run);
+        const float alpha = weight(m_run, mx);
+        s.x = weight(s.x, mx); s.y = weight(s.y, mx); s.z = weight(s.z, mx); s.w = weight(s.w, mx);
+        l_run = l_run * alpha + (s.x + s.y + s.z + s.w);
+        m_run = mx;
+        *reinterpret_cast<float4*>(&sm.s[warp][my_head][(lane & 3) * 4]) = s;
+        if ((lane & 3) == 0) sm.alpha[warp][my_head] = alpha;
+      }
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h)
+        if (h < heads) {
+          const float alpha = sm.alpha[warp][h];
+#pragma unroll
+          for (int c = 0; c < C; ++c) o[h][c] *= alpha;
+        }
+      for (int j = 0; j < 16 && key0 + j < k1; ++j) {
+        const int key = key0 + j, page = page_of(p, seq, key);
+        if (page < 0) continue;
+        float vf[C];
+        load_n<T, C>(vp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + lane * C, vf);
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h)
+          if (h < heads) {
+            const float w = sm.s[warp][h][j];
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[h][c] += w * vf[c];
+          }
+      }
+      __syncwarp();
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+      if (h < heads)
+#pragma unroll
+        for (int c = 0; c < C; ++c) out.o[warp][h][lane * C + c] = o[h][c];
+    l_run += __shfl_xor_sync(~0u, l_run, 1);
+    l_run += __shfl_xor_sync(~0u, l_run, 2);
+    if ((lane & 3) == 0) {
+      out.m[warp][my_head] = m_run;
+      out.l[warp][my_head] = l_run;
+    }
+    __syncthreads();
+  }
+};
+
+// The block that holds unit u when `total` units are spread over n blocks (block c begins at total * c / n).
+__device__ __forceinline__ int block_of(long long u, long long total, int n) { return (int)(((u + 1) * n - 1) / total); }
+
+template <typename T, int DH>
+__device__ __forceinline__ void write_row(const AttendParams& p, int seq, int head, int col, float o, float m, float l) {
+  const int64_t at = (int64_t)seq * p.n_heads + head;
+  ((T*)p.out)[at * DH + col] = from_f<T>(l == 0.f ? 0.f : o / l);     // l = 0: no key at all
+  if (p.lse != nullptr && col == 0) p.lse[at] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) / kLog2e + logf(l);
+}
+
+template <typename T, int DH, typename Item>
+__global__ void __launch_bounds__(kAttThreads) paged_attention_kernel(const __grid_constant__ AttendParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  __shared__ MergeSmem<DH> mg;
+  __shared__ typename Item::Smem sm;
+  __shared__ long long s_sum[kAttWarps], s_before;
+  __shared__ int s_seq, s_last;
+  __shared__ float s_m[kHeads], s_l[kHeads];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int items = p.n_kv * p.head_blocks;
+
+  // Units ahead of every sequence: a thread adds up a run of sequences, a scan over the threads does the rest.
+  const int per = (p.n_seqs + kAttThreads - 1) / kAttThreads;
+  const int s0 = min(tid * per, p.n_seqs), s1 = min(s0 + per, p.n_seqs);
+  long long mine = 0;
+  for (int s = s0; s < s1; ++s) {
+    const int raw = p.lens[s];
+    if ((raw < 0 || raw > p.cap) && p.status != nullptr) *p.status = AMPH_ERR_INVALID_ARG;
+    mine += (clamped_len(p, s) + kUnit - 1) / kUnit;
+  }
+  mine *= items;
+  long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long x = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 31) s_sum[warp] = upto;
+  __syncthreads();
+  long long total = 0, ahead = 0;
+#pragma unroll
+  for (int w = 0; w < kAttWarps; ++w) {
+    if (w < warp) ahead += s_sum[w];
+    total += s_sum[w];
+  }
+  const long long before = ahead + upto - mine;
+
+  // sequences without keys
+  for (int s = blockIdx.x; s < p.n_seqs; s += gridDim.x)
+    if (clamped_len(p, s) == 0)
+      for (int i = tid; i < p.n_heads * DH; i += kAttThreads) write_row<T, DH>(p, s, i / DH, i % DH, 0.f, 0.f, 0.f);
+
+  const int n = (int)(total < gridDim.x ? total : gridDim.x);
+  if ((int)blockIdx.x >= n) return;
+  const long long u0 = total * blockIdx.x / n, u1 = total * (blockIdx.x + 1) / n;
+  if (u0 >= before && u0 < before + mine) {
+    long long at = before;
+    int s = s0;
+    for (;; ++s) {
+      const long long here = (long long)((clamped_len(p, s) + kUnit - 1) / kUnit) * items;
+      if (u0 < at + here) break;
+      at += here;
+    }
+    s_seq = s;
+    s_before = at;
+  }
+  __syncthreads();
+  int seq = s_seq;
+  long long u = u0;
+  int len = clamped_len(p, seq), tiles = (len + kUnit - 1) / kUnit;
+  int item = (int)((u0 - s_before) / tiles), tile = (int)((u0 - s_before) - (long long)item * tiles);
+  while (u < u1) {
+    const int take = (int)(u1 - u < tiles - tile ? u1 - u : tiles - tile);
+    const int kv = item / p.head_blocks, block0 = (item - kv * p.head_blocks) * kHeads;
+    const int head0 = kv * p.group + block0, heads = min(kHeads, p.group - block0);
+    const int k0 = tile * kUnit, k1 = min(len, (tile + take) * kUnit);
+    Item::run(p, sm, mg, seq, kv, head0, heads, k0, k1);
+    const bool whole = take == tiles;
+    const long long first = u - tile;
+    float* part = p.parts + ((size_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * p.part_floats;
+    for (int i = tid; i < heads * DH; i += kAttThreads) {
+      const int h = i / DH, c = i % DH;
+      float m = mg.m[0][h];
+#pragma unroll
+      for (int w = 1; w < kAttWarps; ++w) m = fmaxf(m, mg.m[w][h]);
+      float o = 0.f, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttWarps; ++w) {
+        const float f = weight(mg.m[w][h], m);
+        o += f * mg.o[w][h][c];
+        l += f * mg.l[w][h];
+      }
+      if (whole) {
+        write_row<T, DH>(p, seq, head0 + h, c, o, m, l);
+      } else {
+        part[i] = o;
+        if (c == 0) { part[kHeads * DH + 2 * h] = m; part[kHeads * DH + 2 * h + 1] = l; }
+      }
+    }
+    if (!whole) {
+      const int c0 = block_of(first, total, n), c1 = block_of(first + tiles - 1, total, n);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        s_last = atomicAdd(&p.counters[c0], 1) == c1 - c0;
+        if (s_last) p.counters[c0] = 0;
+      }
+      __syncthreads();
+      if (s_last) {
+        __threadfence();
+        const float* all = p.parts + (size_t)c0 * 2 * p.part_floats;       // block c0 + i: part 1 for i = 0, part 0 behind it
+        for (int h = warp; h < heads; h += kAttWarps) {
+          float m = -INFINITY;
+          for (int c = lane; c <= c1 - c0; c += 32)
+            m = fmaxf(m, __ldcg(all + (size_t)(2 * c + (c == 0)) * p.part_floats + kHeads * DH + 2 * h));
+#pragma unroll
+          for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+          float l = 0.f;
+          for (int c = lane; c <= c1 - c0; c += 32) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(all + (size_t)(2 * c + (c == 0)) * p.part_floats + kHeads * DH + 2 * h));
+            l += ml.y * weight(ml.x, m);
+          }
+#pragma unroll
+          for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
+          if (lane == 0) { s_m[h] = m; s_l[h] = l; }
+        }
+        __syncthreads();
+        for (int i = tid; i < heads * DH; i += kAttThreads) {
+          const int h = i / DH;
+          const float m = s_m[h];
+          float o = 0.f;
+#pragma unroll 8
+          for (int c = 0; c <= c1 - c0; ++c) {
+            const float* x = all + (size_t)(2 * c + (c == 0)) * p.part_floats;
+            o += __ldcg(x + i) * weight(__ldcg(x + kHeads * DH + 2 * h), m);
+          }
+          write_row<T, DH>(p, seq, head0 + h, i % DH, o, m, s_l[h]);
+        }
+      }
+    }
+    u += take;
+    tile += take;
+    if (tile == tiles) {
+      tile = 0;
+      if (++item == items) {
+        item = 0;
+        if (u < u1) {
+          do ++seq; while ((len = clamped_len(p, seq)) == 0);
+          tiles = (len + kUnit - 1) / kUnit;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// AMPH_OK if the cache is one that the kernels take; *shift: log2 of its page size.
+amph_status check_cache(const amph_paged_cache* c, int32_t n_seqs, int32_t table_stride, int* shift) {
+  if (!c || !c->k_pages || !c->v_pages) return api_fail(AMPH_ERR_INVALID_ARG, "cache and its pages must not be NULL");
+  if (c->dtype != AMPH_DTYPE_F32 && c->dtype != AMPH_DTYPE_BF16) return api_fail(AMPH_ERR_SHAPE, "unknown dtype %d", c->dtype);
+  if (c->head_dim != 64 && c->head_dim != 128) return api_fail(AMPH_ERR_SHAPE, "head_dim must be 64 or 128 (got %d)", c->head_dim);
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_pages < 1)
+    return api_fail(AMPH_ERR_SHAPE, "n_kv_heads must be in 1..1024 and n_pages positive");
+  if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
+    return api_fail(AMPH_ERR_SHAPE, "page_size must be a power of two, at most 65536 (got %d)", c->page_size);
+  if (n_seqs < 0 || table_stride < 1) return api_fail(AMPH_ERR_SHAPE, "n_seqs must not be negative and table_stride positive");
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages)) return api_fail(AMPH_ERR_INVALID_ARG, "the pages must be 16-byte aligned");
+  *shift = 0;
+  while ((1 << *shift) < c->page_size) ++*shift;
+  return AMPH_OK;
+}
+
+amph_status launched(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) return AMPH_OK;
+  cudaGetLastError();
+  return api_fail(AMPH_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// theta^(-2 i / dh) / (2 pi) for every pair, kept per thread for the last (theta, dh).
+void fill_turns(float theta, int dh, u64* turn) {
+  struct Kept { float theta = 0.f; int dh = 0; u64 turn[64]; };
+  static thread_local Kept kept;
+  if (kept.theta != theta || kept.dh != dh) {
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    for (int i = 0; i < dh / 2; ++i) {
+      const long double share = powl((long double)theta, -2.0L * i / dh) / two_pi;
+      kept.turn[i] = (u64)((share - floorl(share)) * 18446744073709551616.0L);
+    }
+    kept.theta = theta;
+    kept.dh = dh;
+  }
+  memcpy(turn, kept.turn, sizeof(u64) * (dh / 2));
+}
+
+template <typename TS, typename TD>
+cudaError_t run_write(const WriteParams& p, int rows, cudaStream_t st) {
+  const int items = (p.n_heads + 2 * p.n_kv) * (p.dh / 16);
+  return launch_pdl(paged_write_kernel<TS, TD>, dim3(rows, (items + 2 * kWriteThreads - 1) / (2 * kWriteThreads)), dim3(kWriteThreads), 0, st, p);
+}
+
+template <typename T, int DH, typename Item>
+cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
+  int dev = 0, sms = 0, resident = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, paged_attention_kernel<T, DH, Item>, kAttThreads, 0);
+  if (e != cudaSuccess) return e;
+  int grid = sms * (resident < 1 ? 1 : resident);
+  if (grid > kMaxBlocks) grid = kMaxBlocks;
+  return launch_pdl(paged_attention_kernel<T, DH, Item>, dim3(grid), dim3(kAttThreads), 0, st, p);
+}
+
+static_assert(kMaxBlocks * sizeof(int) <= AMPH_PAGED_WS_COUNTERS, "counters");
+static_assert(AMPH_PAGED_WS_COUNTERS + (size_t)kMaxBlocks * 2 * kHeads * (128 + 2) * sizeof(float) <= AMPH_PAGED_WS_BYTES, "parts");
+
+}  // namespace
+}  // namespace amph
+
+using namespace amph;
+
+extern "C" {
+
+amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                             const void* v, int64_t v_stride, int32_t src_dtype, int32_t n_heads, int32_t rows,
+                             const int32_t* row_seq, const int32_t* row_pos, const int32_t* table, int32_t n_seqs,
+                             int32_t table_stride, float theta, void* q_out, int32_t* status_dev, void* stream) {
+  int shift = 0;
+  const amph_status rc = check_cache(cache, n_seqs, table_stride, &shift);
+  if (rc != AMPH_OK) return rc;
+  if (!k || !v || !row_seq || !row_pos || !table || (n_heads != 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr))
+    return api_fail(AMPH_ERR_INVALID_ARG, "k, v, row_seq, row_pos and table must not be NULL; q and q_out go together, with n_heads > 0");
+  if (src_dtype != AMPH_DTYPE_F32 && src_dtype != AMPH_DTYPE_BF16) return api_fail(AMPH_ERR_SHAPE, "unknown src_dtype %d", src_dtype);
+  if (n_heads < 0 || n_heads > 1024 || rows < 0) return api_fail(AMPH_ERR_SHAPE, "n_heads must be in 0..1024 and rows not negative");
+  if (!(theta > 0.f) || !isfinite(theta)) return api_fail(AMPH_ERR_INVALID_ARG, "theta must be positive and finite");
+  const int dh = cache->head_dim, esz = src_dtype == AMPH_DTYPE_F32 ? 4 : 2;
+  if ((q && q_stride < (int64_t)n_heads * dh) || k_stride < (int64_t)cache->n_kv_heads * dh || v_stride < (int64_t)cache->n_kv_heads * dh)
+    return api_fail(AMPH_ERR_SHAPE, "a row stride is shorter than the row");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || ((q ? q_stride : 0) | k_stride | v_stride) * esz % 16)
+    return api_fail(AMPH_ERR_INVALID_ARG, "q, k, v and q_out must be 16-byte aligned, their row strides multiples of 16 bytes");
+  if (rows == 0) return AMPH_OK;
+  WriteParams p;
+  p.q = q; p.k = k; p.v = v;
+  p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;
+  p.q_out = q_out; p.k_pages = cache->k_pages; p.v_pages = cache->v_pages;
+  p.row_seq = row_seq; p.row_pos = row_pos; p.table = table;
+  p.status = status_dev;
+  p.n_seqs = n_seqs; p.table_stride = table_stride; p.n_heads = n_heads; p.n_kv = cache->n_kv_heads;
+  p.dh = dh; p.page_shift = shift; p.n_pages = cache->n_pages;
+  fill_turns(theta, dh, p.turn);
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool sf = src_dtype == AMPH_DTYPE_F32, df = cache->dtype == AMPH_DTYPE_F32;
+  return launched(sf ? (df ? run_write<float, float>(p, rows, st) : run_write<float, bf16>(p, rows, st))
+                     : (df ? run_write<bf16, float>(p, rows, st) : run_write<bf16, bf16>(p, rows, st)), "amph_paged_write");
+}
+
+amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, int32_t n_heads, const int32_t* lens,
+                                 const int32_t* table, int32_t n_seqs, int32_t table_stride, float scale, void* out, float* lse,
+                                 void* ws_dev, size_t ws_bytes, int32_t ws_clean, int32_t* status_dev, void* stream) {
+  int shift = 0;
+  const amph_status rc = check_cache(cache, n_seqs, table_stride, &shift);
+  if (rc != AMPH_OK) return rc;
+  if (!q || !lens || !table || !out || q == out) return api_fail(AMPH_ERR_INVALID_ARG, "q, lens, table and out must not be NULL, and out not q");
+  if (n_heads < 1 || n_heads > 1024 || n_heads % cache->n_kv_heads)
+    return api_fail(AMPH_ERR_SHAPE, "n_heads (%d) must be a multiple of n_kv_heads (%d), at most 1024", n_heads, cache->n_kv_heads);
+  if (n_seqs > AMPH_PAGED_MAX_SEQS) return api_fail(AMPH_ERR_SHAPE, "n_seqs must be at most %d (got %d)", AMPH_PAGED_MAX_SEQS, n_seqs);
+  if (!isfinite(scale)) return api_fail(AMPH_ERR_INVALID_ARG, "scale must be finite");
+  if (!aligned16(q) || !aligned16(out)) return api_fail(AMPH_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+  if (!ws_dev || ((uintptr_t)ws_dev & 255) || ws_bytes < AMPH_PAGED_WS_BYTES)
+    return api_fail(AMPH_ERR_WORKSPACE, "scratch: %u bytes needed, 256-byte aligned", AMPH_PAGED_WS_BYTES);
+  if (n_seqs == 0) return AMPH_OK;
+  AttendParams p;
+  p.q = q; p.k = cache->k_pages; p.v = cache->v_pages;
+  p.lens = lens; p.table = table; p.out = out; p.lse = lse;
+  p.counters = (int*)ws_dev;
+  p.parts = (float*)((char*)ws_dev + AMPH_PAGED_WS_COUNTERS);
+  p.status = status_dev;
+  p.part_floats = kHeads * (cache->head_dim + 2);
+  p.n_seqs = n_seqs; p.table_stride = table_stride; p.n_heads = n_heads; p.n_kv = cache->n_kv_heads;
+  p.group = n_heads / cache->n_kv_heads;
+  p.head_blocks = (p.group + kHeads - 1) / kHeads;
+  p.page_shift = shift; p.n_pages = cache->n_pages;
+  const int64_t cap = (int64_t)table_stride << shift;
+  p.cap = cap > 0x7fff0000 ? 0x7fff0000 : (int)cap;
+  p.scale_log2 = (scale == 0.f ? 1.0f / sqrtf((float)cache->head_dim) : scale) * kLog2e;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (!ws_clean) {
+    const cudaError_t e = cudaMemsetAsync(ws_dev, 0, AMPH_PAGED_WS_COUNTERS, st);
+    if (e != cudaSuccess) return launched(e, "amph_paged_attention");
+  }
+  const bool d64 = cache->head_dim == 64;
+  if (cache->dtype == AMPH_DTYPE_F32)
+    return launched(d64 ? run_attention<float, 64, PlainItem<float, 64>>(p, st) : run_attention<float, 128, PlainItem<float, 128>>(p, st),
+                    "amph_paged_attention");
+  return launched(d64 ? run_attention<bf16, 64, PlainItem<bf16, 64>>(p, st) : run_attention<bf16, 128, PlainItem<bf16, 128>>(p, st),
+                  "amph_paged_attention");
+}
+
+}  // extern "C"
