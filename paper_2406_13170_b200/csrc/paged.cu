@@ -10,8 +10,6 @@ namespace {
 
 typedef __nv_bfloat16 bf16;
 
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
 template <typename T> __device__ __forceinline__ T from_f(float v);
 template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
@@ -139,6 +137,7 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid
 constexpr int kUnit = 64;                // keys: 16 for each warp
 constexpr int kAttWarps = 4;
 constexpr int kAttThreads = kAttWarps * 32;
+constexpr int kAttResident = 3;          // blocks per SM: 168 registers a thread
 constexpr int kHeads = 8;                // query heads of an item
 constexpr int kMaxBlocks = 592;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -179,26 +178,17 @@ __device__ __forceinline__ int page_of(const AttendParams& p, int seq, int key) 
   return -1;
 }
 
-template <typename T, int N>
-__device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
-  if constexpr (sizeof(T) == 4 && N == 4) {
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  } else if constexpr (sizeof(T) == 4) {
-    const float2 a = *reinterpret_cast<const float2*>(p);
-    v[0] = a.x; v[1] = a.y;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      const uint32_t u = *reinterpret_cast<const uint32_t*>(p + i);
-      v[i] = __uint_as_float(u << 16);
-      v[i + 1] = __uint_as_float(u & 0xffff0000u);
-    }
-  }
+__device__ __forceinline__ void load_n(const float* p, float (&v)[4]) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+}
+__device__ __forceinline__ void load_n(const float* p, float (&v)[2]) {
+  const float2 a = *reinterpret_cast<const float2*>(p);
+  v[0] = a.x; v[1] = a.y;
 }
 
-// Keys [k0, k1) of one item by CUDA cores: scores with eight lanes per key, weighted values with every lane on its own columns.
-template <typename T, int DH>
+// Keys [k0, k1) of one fp32 item by CUDA cores: scores with eight lanes per key, weighted values with every lane on its own columns.
+template <int DH>
 struct PlainItem {
   struct Smem {
     float q[kHeads][DH];
@@ -209,10 +199,10 @@ struct PlainItem {
     constexpr int C = DH / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     for (int i = tid; i < heads * DH; i += kAttThreads)
-      sm.q[i / DH][i % DH] = to_f(((const T*)p.q)[((int64_t)seq * p.n_heads + head0) * DH + i]);
+      sm.q[i / DH][i % DH] = ((const float*)p.q)[((int64_t)seq * p.n_heads + head0) * DH + i];
     __syncthreads();
-    const T* kp = (const T*)p.k;
-    const T* vp = (const T*)p.v;
+    const float* kp = (const float*)p.k;
+    const float* vp = (const float*)p.v;
     const int page_mask = (1 << p.page_shift) - 1;
     float o[kHeads][C];
 #pragma unroll
@@ -230,7 +220,7 @@ struct PlainItem {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           if (page >= 0)
-            load_n<T, 4>(kp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + c * 32 + (lane & 7) * 4, kf[c]);
+            load_n(kp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + c * 32 + (lane & 7) * 4, kf[c]);
           else
             kf[c][0] = kf[c][1] = kf[c][2] = kf[c][3] = 0.f;
         }
@@ -274,7 +264,7 @@ struct PlainItem {
         const int key = key0 + j, page = page_of(p, seq, key);
         if (page < 0) continue;
         float vf[C];
-        load_n<T, C>(vp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + lane * C, vf);
+        load_n(vp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + lane * C, vf);
 #pragma unroll
         for (int h = 0; h < kHeads; ++h)
           if (h < heads) {
@@ -300,6 +290,167 @@ struct PlainItem {
   }
 };
 
+__device__ __forceinline__ uint4 load_once(const bf16* p) {          // 16 bytes that no other thread of the block reads
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Keys [k0, k1) of one bf16 item on the warp-level tensor cores, 16 keys of a warp at a time, straight from the pages to registers:
+// no shared memory, no barrier, the next 16 keys' loads in flight while these are worked on.
+//   Scores   S[head][key]: A = queries (rows 0-7; rows 8-15 zero), B = keys.  The sum over head_dim may run in any order that both
+//            operands share, so a lane takes 16 contiguous bytes of its key for two steps.
+//   Values   O[head][column]: A = weights, B = values.  Rows 8-15 carry what the weights of rows 0-7 lose when they are rounded to
+//            bf16, so 16 bits of every weight enter at no further cost; columns may be numbered in any order, so a lane takes 16
+//            contiguous bytes of four keys and pairs them with byte permutes.
+// Bound: HBM.  A key's 4 head_dim bytes cost at most 16 head_dim * 4 flops, a tenth of what the tensor pipe does meanwhile.
+template <int DH>
+struct MmaItem {
+  struct Smem {};
+  static __device__ __forceinline__ void run(const AttendParams& p, Smem&, MergeSmem<DH>& out, int seq, int kv, int head0, int heads, int k0, int k1) {
+    constexpr int C = DH / 32, H = DH / 64;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const bf16* kp = (const bf16*)p.k;
+    const bf16* vp = (const bf16*)p.v;
+    const bool wide = p.page_shift >= 4;             // 16 keys share a page
+    const int page_mask = (1 << p.page_shift) - 1;
+    uint4 q[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) q[c] = make_uint4(0u, 0u, 0u, 0u);
+    if (g < heads) {
+      const bf16* qp = (const bf16*)p.q + ((int64_t)seq * p.n_heads + head0 + g) * DH + t * 8;
+#pragma unroll
+      for (int c = 0; c < C; ++c) q[c] = *reinterpret_cast<const uint4*>(qp + c * 32);
+    }
+    float o[H][8][4];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // lane j (and j + 16) knows the page of key j of the 16 at `key0`; -1: none
+    auto find = [&](int key0) {
+      const int key = key0 + (lane & 15);
+      return key < k1 ? page_of(p, seq, key) : -1;
+    };
+    // element offset of key j's row, and which keys of the 16 there are
+    auto row_of = [&](int key0, int page, int j) {
+      const int from = __shfl_sync(~0u, page, wide ? 0 : j);
+      return ((((int64_t)from * p.n_kv + kv) << p.page_shift) + ((key0 + j) & page_mask)) * DH;
+    };
+    uint4 kr[2][C], vr[4][H];
+    auto load_k = [&](int key0, int page, unsigned there) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int j = n * 8 + g;
+        const bf16* src = kp + row_of(key0, page, j) + t * 8;
+#pragma unroll
+        for (int c = 0; c < C; ++c) kr[n][c] = (there >> j) & 1 ? load_once(src + c * 32) : make_uint4(0u, 0u, 0u, 0u);
+      }
+    };
+    auto load_v = [&](int key0, int page, unsigned there) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = 2 * t + (i & 1) + (i >> 1) * 8;
+        const bf16* src = vp + row_of(key0, page, j) + g * 8;
+#pragma unroll
+        for (int h = 0; h < H; ++h) vr[i][h] = (there >> j) & 1 ? load_once(src + h * 64) : make_uint4(0u, 0u, 0u, 0u);
+      }
+    };
+    int key0 = k0 + warp * 16;
+    int page = find(key0);
+    unsigned there = __ballot_sync(~0u, page >= 0);
+    load_k(key0, page, there);
+    load_v(key0, page, there);
+    int page_next = find(key0 + kUnit);
+    for (; key0 < k1; key0 += kUnit) {
+      float s[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          mma_16816(s[n], q[c].x, 0u, q[c].y, 0u, kr[n][c].x, kr[n][c].y);
+          mma_16816(s[n], q[c].z, 0u, q[c].w, 0u, kr[n][c].z, kr[n][c].w);
+        }
+      }
+      const unsigned now = there;
+      there = __ballot_sync(~0u, page_next >= 0);
+      load_k(key0 + kUnit, page_next, there);
+      float w[2][2];
+      float mx = m_run;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          w[n][i] = (now >> (n * 8 + 2 * t + i)) & 1 ? s[n][i] * p.scale_log2 : -INFINITY;
+          mx = fmaxf(mx, w[n][i]);
+        }
+      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
+      if (__any_sync(~0u, mx != m_run)) {
+        const float alpha = weight(m_run, mx);
+        l_run *= alpha;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[h][j][i] *= alpha;
+        m_run = mx;
+      }
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        w[n][0] = weight(w[n][0], mx);
+        w[n][1] = weight(w[n][1], mx);
+        l_run += w[n][0] + w[n][1];
+        hi[n] = pack(w[n][0], w[n][1]);
+        lo[n] = pack(w[n][0] - __uint_as_float(hi[n] << 16), w[n][1] - __uint_as_float(hi[n] & 0xffff0000u));
+      }
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const uint32_t v[4][4] = {{vr[0][h].x, vr[0][h].y, vr[0][h].z, vr[0][h].w}, {vr[1][h].x, vr[1][h].y, vr[1][h].z, vr[1][h].w},
+                                  {vr[2][h].x, vr[2][h].y, vr[2][h].z, vr[2][h].w}, {vr[3][h].x, vr[3][h].y, vr[3][h].z, vr[3][h].w}};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t pick = j & 1 ? 0x7632u : 0x5410u;
+          mma_16816(o[h][j], hi[0], lo[0], hi[1], lo[1], __byte_perm(v[0][j >> 1], v[1][j >> 1], pick), __byte_perm(v[2][j >> 1], v[3][j >> 1], pick));
+        }
+      }
+      load_v(key0 + kUnit, page_next, there);
+      page_next = find(key0 + 2 * kUnit);
+    }
+    l_run += __shfl_xor_sync(~0u, l_run, 1);
+    l_run += __shfl_xor_sync(~0u, l_run, 2);
+    if (g < heads) {
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; j += 4)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<float4*>(&out.o[warp][g][h * 64 + t * 16 + i * 8 + j]) =
+                make_float4(o[h][j][i] + o[h][j][i + 2], o[h][j + 1][i] + o[h][j + 1][i + 2], o[h][j + 2][i] + o[h][j + 2][i + 2],
+                            o[h][j + 3][i] + o[h][j + 3][i + 2]);
+      if (t == 0) {
+        out.m[warp][g] = m_run;
+        out.l[warp][g] = l_run;
+      }
+    }
+    __syncthreads();
+  }
+};
+
 // The block that holds unit u when `total` units are spread over n blocks (block c begins at total * c / n).
 __device__ __forceinline__ int block_of(long long u, long long total, int n) { return (int)(((u + 1) * n - 1) / total); }
 
@@ -311,7 +462,7 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int seq, int he
 }
 
 template <typename T, int DH, typename Item>
-__global__ void __launch_bounds__(kAttThreads) paged_attention_kernel(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_kernel(const __grid_constant__ AttendParams p) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ MergeSmem<DH> mg;
@@ -505,12 +656,11 @@ cudaError_t run_write(const WriteParams& p, int rows, cudaStream_t st) {
 
 template <typename T, int DH, typename Item>
 cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
-  int dev = 0, sms = 0, resident = 0;
+  int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, paged_attention_kernel<T, DH, Item>, kAttThreads, 0);
   if (e != cudaSuccess) return e;
-  int grid = sms * (resident < 1 ? 1 : resident);
+  int grid = sms * kAttResident;
   if (grid > kMaxBlocks) grid = kMaxBlocks;
   return launch_pdl(paged_attention_kernel<T, DH, Item>, dim3(grid), dim3(kAttThreads), 0, st, p);
 }
@@ -594,9 +744,9 @@ amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, i
   }
   const bool d64 = cache->head_dim == 64;
   if (cache->dtype == AMPH_DTYPE_F32)
-    return launched(d64 ? run_attention<float, 64, PlainItem<float, 64>>(p, st) : run_attention<float, 128, PlainItem<float, 128>>(p, st),
+    return launched(d64 ? run_attention<float, 64, PlainItem<64>>(p, st) : run_attention<float, 128, PlainItem<128>>(p, st),
                     "amph_paged_attention");
-  return launched(d64 ? run_attention<bf16, 64, PlainItem<bf16, 64>>(p, st) : run_attention<bf16, 128, PlainItem<bf16, 128>>(p, st),
+  return launched(d64 ? run_attention<bf16, 64, MmaItem<64>>(p, st) : run_attention<bf16, 128, MmaItem<128>>(p, st),
                   "amph_paged_attention");
 }
 
