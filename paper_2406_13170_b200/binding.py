@@ -434,17 +434,6 @@ def _want(t: torch.Tensor, name: str, device: torch.device, dtype, shape=None) -
     return t
 
 
-def _call(L, fn, index: int, args) -> None:
-    """fn(*args, current stream) with device `index` current."""
-    if torch.cuda.current_device() == index:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
-    else:
-        with torch.cuda.device(index):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
-    if rc != 0:
-        raise AmphError(rc, L.amph_last_error(None).decode())
-
-
 class Adapters:
     """Low-rank adapters of a projection with n_seg weight matrices (amph_adapters).
 
@@ -468,22 +457,35 @@ class Adapters:
         if scale is not None:
             _want(scale, "scale", a.device, torch.float32, (self.n,))
         self.tensors = (a, b, scale)
+        self.index = a.device.index
+        self.w_shape = (self.out, self.in_)
+        self.w_array = C.c_void_p * self.n_seg
         self.c = amph_adapters(a.data_ptr(), b.data_ptr(), None if scale is None else scale.data_ptr(), self.n, self.rank)
+        self.ref = C.byref(self.c)
+        self._bytes: Dict[int, int] = {}
+
+    def scratch_bytes(self, rows: int) -> int:
+        """amph_project_adapters_bytes for this many rows."""
+        need = self._bytes.get(rows)
+        if need is None:
+            L, n = lib(), C.c_size_t()
+            rc = L.amph_project_adapters_bytes(self.n_seg, self.out, rows, self.rank, C.byref(n))
+            if rc != 0:
+                raise AmphError(rc, L.amph_last_error(None).decode())
+            need = self._bytes[rows] = n.value
+        return need
 
 
-def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use_tensor_core: bool, adapters: Adapters,
-                     row_adapter: torch.Tensor, y: Optional[torch.Tensor] = None, y_dtype: Optional[torch.dtype] = None,
-                     status: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """amph_project_adapters: y[r] = x[r] . W^T + scale (x[r] . a^T) . b^T with the adapter row_adapter[r] (int32 [rows], < 0: none).
-
-    x, ws, rows, use_tensor_core as for `project`; y [rows, n_seg * out] of y_dtype (default: x's type)."""
-    L = lib()
+def _check_adapters_call(x, ws, rows, adapters, row_adapter, y, y_dtype, status):
+    """Says what is wrong with a call of project_adapters (everything that the library cannot see from addresses)."""
     n_seg, dev, dt = len(ws), x.device, x.dtype
     if dt not in _DTYPES or x.dim() != 2 or n_seg < 1:
         _refuse(2, f"x must be a float32 or bfloat16 matrix (got {dt}, {tuple(x.shape)}), with at least one weight matrix")
     if not x.is_cuda:
         _refuse(7, "x must be on a CUDA device")
     _want(x, "x", dev, dt)
+    if ws[0].dim() != 2:
+        _refuse(2, f"w must be a matrix (got {tuple(ws[0].shape)})")
     out, in_ = ws[0].shape
     for w in ws:
         _want(w, "w", dev, dt, (out, in_))
@@ -493,26 +495,46 @@ def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use
     if adapters.dtype is not dt or adapters.device != dev:
         _refuse(1, f"the adapters are {adapters.dtype} on {adapters.device}, x is {dt} on {dev}")
     _want(row_adapter, "row_adapter", dev, torch.int32, (rows,))
-    if y is None:
-        y = torch.empty(rows, n_seg * out, dtype=y_dtype or dt, device=dev)
-    else:
+    if y is not None:
         if y_dtype is not None and y.dtype is not y_dtype:
             _refuse(1, f"y is {y.dtype}, not {y_dtype}")
         _want(y, "y", dev, y.dtype, (rows, n_seg * out))
-    if y.dtype not in _DTYPES:
-        _refuse(2, f"y must be float32 or bfloat16 (got {y.dtype})")
+    if (y_dtype if y is None else y.dtype) not in (None, *_DTYPES):
+        _refuse(2, "y must be float32 or bfloat16")
     if status is not None:
         _want(status, "status", dev, torch.int32)
-    need = C.c_size_t()
-    rc = L.amph_project_adapters_bytes(n_seg, out, rows, adapters.rank, C.byref(need))
+
+
+def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use_tensor_core: bool, adapters: Adapters,
+                     row_adapter: torch.Tensor, y: Optional[torch.Tensor] = None, y_dtype: Optional[torch.dtype] = None,
+                     status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """amph_project_adapters: y[r] = x[r] . W^T + scale (x[r] . a^T) . b^T with the adapter row_adapter[r] (int32 [rows], < 0: none).
+
+    x, ws, rows, use_tensor_core as for `project`; y [rows, n_seg * out] of y_dtype (default: x's type)."""
+    n_seg, index, dt = adapters.n_seg, adapters.index, adapters.dtype
+    ok = (len(ws) == n_seg and x.dim() == 2 and x.dtype is dt and x.get_device() == index and x.is_contiguous()
+          and row_adapter.dtype is torch.int32 and row_adapter.get_device() == index and row_adapter.shape == (rows,)
+          and row_adapter.is_contiguous() and x.shape[1] == adapters.in_ and y is None and y_dtype is None and status is None)
+    if ok:
+        for w in ws:
+            ok = ok and w.dtype is dt and w.get_device() == index and w.shape == adapters.w_shape and w.is_contiguous()
+    if not ok:
+        _check_adapters_call(x, ws, rows, adapters, row_adapter, y, y_dtype, status)
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return project_adapters(x, ws, rows, use_tensor_core, adapters, row_adapter, y, y_dtype, status)
+    L = lib()
+    out, in_ = adapters.w_shape
+    if y is None:
+        y = torch.empty((rows, n_seg * out), dtype=y_dtype or dt, device=adapters.device)
+    need = adapters.scratch_bytes(rows)
+    scratch = torch.empty(need, dtype=torch.uint8, device=adapters.device)
+    arr = adapters.w_array(*[w.data_ptr() for w in ws])
+    rc = L.amph_project_adapters(x.data_ptr(), x.shape[0], arr, n_seg, out, in_, rows, _DTYPES[dt], int(use_tensor_core), adapters.ref,
+                                 row_adapter.data_ptr(), y.data_ptr(), _DTYPES[y.dtype], scratch.data_ptr(), need,
+                                 None if status is None else status.data_ptr(), torch._C._cuda_getCurrentRawStream(index))
     if rc != 0:
         raise AmphError(rc, L.amph_last_error(None).decode())
-    scratch = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    arr = (C.c_void_p * n_seg)(*[w.data_ptr() for w in ws])
-    _call(L, L.amph_project_adapters, dev.index,
-          (x.data_ptr(), x.shape[0], arr, n_seg, out, in_, rows, _DTYPES[dt], int(use_tensor_core), C.byref(adapters.c),
-           row_adapter.data_ptr(), y.data_ptr(), _DTYPES[y.dtype], scratch.data_ptr(), need.value,
-           None if status is None else status.data_ptr()))
     return y
 
 
@@ -533,25 +555,27 @@ class PagedCache:
         self.c = amph_paged_cache(k_pages.data_ptr(), v_pages.data_ptr(), _DTYPES[self.dtype], self.n_kv_heads, self.head_dim,
                                   self.page_size, self.n_pages)
         self.ref = C.byref(self.c)
+        self.index = self.device.index
 
-    def _table(self, table: torch.Tensor) -> torch.Tensor:
+    def _table(self, table: torch.Tensor) -> None:
         if table.dim() != 2:
             _refuse(2, f"table must be [n_seqs, width] (got {tuple(table.shape)})")
-        return _want(table, "table", self.device, torch.int32)
+        _want(table, "table", self.device, torch.int32)
 
 
 def _rows_of(t: torch.Tensor, name: str, cache: PagedCache, rows: int, heads: int, dtype) -> int:
     """Checks [rows, heads * head_dim] or [rows, heads, head_dim] whose rows are contiguous; returns the row stride in elements."""
-    if t.dtype is not dtype or t.device != cache.device:
-        _refuse(1, f"{name} must be {dtype} on {cache.device} (got {t.dtype} on {t.device})")
     dh = cache.head_dim
-    if t.dim() == 2:
-        fits = t.shape[0] == rows and t.shape[1] == heads * dh and t.stride(1) == 1
+    stride = t.stride()
+    if len(stride) == 2:
+        fits = t.shape == (rows, heads * dh) and stride[1] == 1
     else:
-        fits = t.dim() == 3 and t.shape == (rows, heads, dh) and t.stride(2) == 1 and (t.stride(1) == dh or heads == 1)
+        fits = t.shape == (rows, heads, dh) and stride[2] == 1 and (stride[1] == dh or heads == 1)
+    if t.dtype is not dtype or t.get_device() != cache.index:
+        _refuse(1, f"{name} must be {dtype} on {cache.device} (got {t.dtype} on {t.device})")
     if not fits:
-        _refuse(2, f"{name} must be {rows} rows of {heads} heads of {dh}, each row contiguous (got {tuple(t.shape)}, strides {t.stride()})")
-    return t.stride(0) if rows > 1 else heads * dh
+        _refuse(2, f"{name} must be {rows} rows of {heads} heads of {dh}, each row contiguous (got {tuple(t.shape)}, strides {stride})")
+    return stride[0] if rows > 1 else heads * dh
 
 
 def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, row_seq: torch.Tensor,
@@ -561,31 +585,41 @@ def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v
 
     q [rows, n_heads * head_dim] (or None), k, v [rows, n_kv_heads * head_dim], fp32 or bf16 (one type), each row contiguous (slices
     of a projection's output); row_seq, row_pos int32 [rows], row_seq < 0: the row is skipped (its place in a new q_out is not set)."""
-    L = lib()
-    dev, rows = cache.device, k.shape[0]
-    if k.dtype not in _DTYPES:
-        _refuse(2, f"k must be float32 or bfloat16 (got {k.dtype})")
-    ks = _rows_of(k, "k", cache, rows, cache.n_kv_heads, k.dtype)
-    vs = _rows_of(v, "v", cache, rows, cache.n_kv_heads, k.dtype)
+    index, rows, dt = cache.index, k.shape[0], k.dtype
+    if dt not in _DTYPES:
+        _refuse(2, f"k must be float32 or bfloat16 (got {dt})")
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return paged_write(cache, q, k, v, row_seq, row_pos, table, theta, q_out, status)
+    ks = _rows_of(k, "k", cache, rows, cache.n_kv_heads, dt)
+    vs = _rows_of(v, "v", cache, rows, cache.n_kv_heads, dt)
     heads = qs = 0
     if q is not None:
         heads = (q.shape[1] * q.shape[2] if q.dim() == 3 else q.shape[-1]) // cache.head_dim
-        qs = _rows_of(q, "q", cache, rows, heads, k.dtype)
+        qs = _rows_of(q, "q", cache, rows, heads, dt)
         if q_out is None:
-            q_out = torch.empty(rows, heads, cache.head_dim, dtype=cache.dtype, device=dev)
-        else:
-            _want(q_out, "q_out", dev, cache.dtype, (rows, heads, cache.head_dim))
+            q_out = torch.empty(rows, heads, cache.head_dim, dtype=cache.dtype, device=cache.device)
+        elif not (q_out.dtype is cache.dtype and q_out.get_device() == index and q_out.shape == (rows, heads, cache.head_dim) and q_out.is_contiguous()):
+            _want(q_out, "q_out", cache.device, cache.dtype, (rows, heads, cache.head_dim))
     elif q_out is not None:
         _refuse(1, "q_out without q")
-    _want(row_seq, "row_seq", dev, torch.int32, (rows,))
-    _want(row_pos, "row_pos", dev, torch.int32, (rows,))
-    cache._table(table)
+    shape = (rows,)
+    if not (row_seq.dtype is torch.int32 and row_pos.dtype is torch.int32 and table.dtype is torch.int32 and row_seq.shape == shape
+            and row_pos.shape == shape and table.dim() == 2 and row_seq.get_device() == index and row_pos.get_device() == index
+            and table.get_device() == index and row_seq.is_contiguous() and row_pos.is_contiguous() and table.is_contiguous()):
+        _want(row_seq, "row_seq", cache.device, torch.int32, shape)
+        _want(row_pos, "row_pos", cache.device, torch.int32, shape)
+        cache._table(table)
     if status is not None:
-        _want(status, "status", dev, torch.int32)
-    _call(L, L.amph_paged_write, dev.index,
-          (cache.ref, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[k.dtype], heads, rows,
-           row_seq.data_ptr(), row_pos.data_ptr(), table.data_ptr(), table.shape[0], table.shape[1], theta,
-           None if q is None else q_out.data_ptr(), None if status is None else status.data_ptr()))
+        _want(status, "status", cache.device, torch.int32)
+    L = lib()
+    n_seqs, width = table.shape
+    rc = L.amph_paged_write(cache.ref, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[dt], heads, rows,
+                            row_seq.data_ptr(), row_pos.data_ptr(), table.data_ptr(), n_seqs, width, theta,
+                            None if q is None else q_out.data_ptr(), None if status is None else status.data_ptr(),
+                            torch._C._cuda_getCurrentRawStream(index))
+    if rc != 0:
+        raise AmphError(rc, L.amph_last_error(None).decode())
     return q_out
 
 
@@ -600,39 +634,41 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, len
 
     The scratch belongs to the stream that the call runs on: one piece per stream, kept; a call that is captured into a
     graph has its own, from the graph's memory."""
-    dev = cache.device
-    index = dev.index
+    index, dt = cache.index, cache.dtype
     if torch.cuda.current_device() != index:
         with torch.cuda.device(index):
             return paged_attention(cache, q, table, lens, scale, out, lse, status)
-    L = lib()
-    if q.dim() != 3:
-        _refuse(2, f"q must be [n_seqs, n_heads, head_dim] (got {tuple(q.shape)})")
-    n, heads, dh = q.shape
-    _want(q, "q", dev, cache.dtype, (n, heads, cache.head_dim))
-    cache._table(table)
-    if table.shape[0] != n:
-        _refuse(2, f"table has {table.shape[0]} rows for {n} sequences")
-    _want(lens, "lens", dev, torch.int32, (n,))
+    shape = q.shape
+    n, heads = (shape[0], shape[1]) if len(shape) == 3 else (0, 0)
+    if not (len(shape) == 3 and shape[2] == cache.head_dim and q.dtype is dt and lens.dtype is torch.int32 and table.dtype is torch.int32
+            and lens.shape == (n,) and table.dim() == 2 and table.shape[0] == n and q.get_device() == index and lens.get_device() == index
+            and table.get_device() == index and q.is_contiguous() and lens.is_contiguous() and table.is_contiguous()):
+        if len(shape) != 3:
+            _refuse(2, f"q must be [n_seqs, n_heads, head_dim] (got {tuple(shape)})")
+        _want(q, "q", cache.device, dt, (n, heads, cache.head_dim))
+        cache._table(table)
+        if table.shape[0] != n:
+            _refuse(2, f"table has {table.shape[0]} rows for {n} sequences")
+        _want(lens, "lens", cache.device, torch.int32, (n,))
     if out is None:
         out = torch.empty_like(q)
     else:
-        _want(out, "out", dev, cache.dtype, q.shape)
+        _want(out, "out", cache.device, dt, shape)
     if lse is not None:
-        _want(lse, "lse", dev, torch.float32, (n, heads))
+        _want(lse, "lse", cache.device, torch.float32, (n, heads))
     if status is not None:
-        _want(status, "status", dev, torch.int32)
-    clean = 0
+        _want(status, "status", cache.device, torch.int32)
+    stream = torch._C._cuda_getCurrentRawStream(index)
     if torch.cuda.is_current_stream_capturing():
-        scratch = torch.empty(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=dev)
+        scratch, clean = torch.empty(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=cache.device), 0
     else:
-        key = (index, torch._C._cuda_getCurrentRawStream(index))
-        scratch = _attention_scratch.get(key)
-        clean = 1
+        scratch, clean = _attention_scratch.get((index, stream)), 1
         if scratch is None:
-            scratch = _attention_scratch[key] = torch.zeros(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=dev)
-    _call(L, L.amph_paged_attention, index,
-          (cache.ref, q.data_ptr(), heads, lens.data_ptr(), table.data_ptr(), n, table.shape[1], scale, out.data_ptr(),
-           None if lse is None else lse.data_ptr(), scratch.data_ptr(), AMPH_PAGED_WS_BYTES, clean,
-           None if status is None else status.data_ptr()))
+            scratch = _attention_scratch[(index, stream)] = torch.zeros(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=cache.device)
+    L = lib()
+    rc = L.amph_paged_attention(cache.ref, q.data_ptr(), heads, lens.data_ptr(), table.data_ptr(), n, table.shape[1], scale, out.data_ptr(),
+                                None if lse is None else lse.data_ptr(), scratch.data_ptr(), AMPH_PAGED_WS_BYTES, clean,
+                                None if status is None else status.data_ptr(), stream)
+    if rc != 0:
+        raise AmphError(rc, L.amph_last_error(None).decode())
     return out

@@ -18,7 +18,6 @@ typedef __nv_bfloat16 bf16;
 constexpr int kMaxRowsAll = 4 * kMaxRows;
 constexpr int kThreads = 128;
 
-__device__ __forceinline__ void put(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // Up to kTileRows rows of one adapter (or without any: adapter < 0), as adapter_down leaves them for adapter_up.
 constexpr int kTileRows = 16;
@@ -32,7 +31,8 @@ struct AdapterArgs {
   const float* scale;
   const int* row_adapter;
   RowTile* tiles;
-  float* t;                // [splits][rows][n_seg * rank]
+  float* t;                // fp32: [rows][n_seg * rank]
+  bf16 *t_hi, *t_lo;       // bf16: the same, times scale, in two halves
   void* y;
   int* status;
   int n_adapters, rank, n_seg, out, in, rows, splits;
@@ -102,128 +102,221 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Tile `tile` of the call's rows: the rows of one adapter in their order, 16 at a time, tiles in the order of their first rows.  Every
+// Tile `want` of the call's rows: the rows of one adapter in their order, 16 at a time, tiles in the order of their first rows.  Every
 // block finds its own (an adapter's rows may lie anywhere): row r is the c-th of its adapter, c = how many rows ahead of it name the same.
-struct TileSmem {
-  int adapter[kMaxRowsAll];
-  short nth[kMaxRowsAll];
-  int firsts[kMaxRowsAll / 32];
-  int leader;
-  RowTile tile;
+// The adapters get slots of a hash table (twice as many as rows), a strip of 32 rows counts its own per slot, a row adds up the strips
+// ahead of its own.  (Comparing every row with all rows ahead of it: 4.7 us more per block at 512 rows, the same at 64.)
+constexpr int kStrips = kMaxRowsAll / 32, kSlots = 2 * kMaxRowsAll;
+struct __align__(16) TileSmem {
+  uint8_t count[kSlots][kStrips];
+  int key[kSlots];
+  short slot[kMaxRowsAll], nth[kMaxRowsAll];
+  int firsts[kStrips];
 };
-__device__ __forceinline__ bool find_tile(const AdapterArgs& p, int tile, TileSmem& sm) {
+static_assert(kStrips == 16, "a slot's counts are one 16-byte word");
+constexpr int kDownThreads = 256, kDownWarps = kDownThreads / 32;
+__device__ __forceinline__ bool find_tile(const AdapterArgs& p, int want, TileSmem& sm, RowTile& tile, int& leader) {
+  constexpr int kNoKey = -2;                 // (adapter_of() answers -1 or more)
+  constexpr int kPer = kMaxRowsAll / kDownThreads;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  for (int r = tid; r < p.rows; r += kThreads) sm.adapter[r] = adapter_of(p, r);
-  if (tid == 0) { sm.leader = -1; sm.tile.n = 0; }
-  __syncthreads();
-  unsigned first[kMaxRowsAll / kThreads];
+  const unsigned ahead = (1u << lane) - 1u;
+  int slots = 64;
+  while (slots < 2 * p.rows) slots *= 2;
+  int adapter[kPer];
 #pragma unroll
-  for (int i = 0; i < kMaxRowsAll / kThreads; ++i) {
-    const int r = i * kThreads + tid;
-    first[i] = 0;
-    if (i * kThreads >= p.rows) break;
-    int c = 0, q = 0;
-    if (r < p.rows) {
-      const int a = sm.adapter[r];
-      for (; q + 4 <= r; q += 4) {
-        const int4 v = *reinterpret_cast<const int4*>(&sm.adapter[q]);
-        c += (v.x == a) + (v.y == a) + (v.z == a) + (v.w == a);
+  for (int i = 0; i < kPer; ++i) {
+    const int r = i * kDownThreads + tid;
+    adapter[i] = r < p.rows ? adapter_of(p, r) : kNoKey;
+  }
+  for (int i = tid; i < slots; i += kDownThreads) {
+    sm.key[i] = kNoKey;
+    *reinterpret_cast<uint4*>(sm.count[i]) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (tid == 0) { leader = -1; tile.n = 0; tile.adapter = -1; }
+  __syncthreads();
+  unsigned same[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int strip = i * kDownWarps + warp;
+    if (strip * 32 >= p.rows) break;
+    same[i] = __match_any_sync(~0u, adapter[i]);
+    const int first = __ffs(same[i]) - 1;
+    int at = 0;
+    if (lane == first && adapter[i] != kNoKey) {
+      at = (int)((uint32_t)adapter[i] * 2654435769u >> 16) & (slots - 1);
+      for (;;) {
+        const int was = atomicCAS(&sm.key[at], kNoKey, adapter[i]);
+        if (was == kNoKey || was == adapter[i]) break;
+        at = (at + 1) & (slots - 1);
       }
-      for (; q < r; ++q) c += sm.adapter[q] == a;
+      sm.count[at][strip] = (uint8_t)__popc(same[i]);
+    }
+    at = __shfl_sync(~0u, at, first);
+    sm.slot[strip * 32 + lane] = (short)at;              // (rows behind the last: not read)
+  }
+  __syncthreads();
+  unsigned firsts[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int strip = i * kDownWarps + warp, r = strip * 32 + lane;
+    firsts[i] = 0;
+    if (strip * 32 >= p.rows) break;
+    int c = __popc(same[i] & ahead);
+    if (r < p.rows) {
+      const uint4 n = *reinterpret_cast<const uint4*>(sm.count[sm.slot[r]]);
+      const unsigned words[4] = {n.x, n.y, n.z, n.w};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int left = strip - 4 * w;                  // strips of this word that are ahead
+        const unsigned mask = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+        c = (int)__dp4a(words[w] & mask, 0x01010101u, (unsigned)c);
+      }
       sm.nth[r] = (short)c;
     }
-    first[i] = __ballot_sync(~0u, r < p.rows && c % kTileRows == 0);
-    if (lane == 0) sm.firsts[i * (kThreads / 32) + warp] = __popc(first[i]);
+    firsts[i] = __ballot_sync(~0u, r < p.rows && c % kTileRows == 0);
+    if (lane == 0) sm.firsts[strip] = __popc(firsts[i]);
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kMaxRowsAll / kThreads; ++i) {
-    if (i * kThreads >= p.rows) break;
-    if ((first[i] >> lane) & 1) {
-      int at = __popc(first[i] & ((1u << lane) - 1u));
-      for (int w = 0; w < i * (kThreads / 32) + warp; ++w) at += sm.firsts[w];
-      if (at == tile) sm.leader = i * kThreads + tid;
+  for (int i = 0; i < kPer; ++i) {
+    const int strip = i * kDownWarps + warp;
+    if ((firsts[i] >> lane) & 1) {
+      int at = __popc(firsts[i] & ahead);
+      for (int w = 0; w < strip; ++w) at += sm.firsts[w];
+      if (at == want) leader = strip * 32 + lane;
     }
+    if (strip * 32 >= p.rows) break;
   }
   __syncthreads();
-  const int leader = sm.leader;
-  if (leader < 0) return false;
-  const int a = sm.adapter[leader], c0 = sm.nth[leader];
-  for (int r = tid; r < p.rows; r += kThreads) {
+  const int lead = leader;
+  if (lead < 0) return false;
+  const int slot = sm.slot[lead], c0 = sm.nth[lead];
+  if (tid == 0) tile.adapter = sm.key[slot];
+  for (int r = tid; r < p.rows; r += kDownThreads) {
     const int c = sm.nth[r] - c0;
-    if (sm.adapter[r] == a && c >= 0 && c < kTileRows) {
-      sm.tile.row[c] = (uint16_t)r;
-      atomicMax(&sm.tile.n, c + 1);
+    if (sm.slot[r] == slot && c >= 0 && c < kTileRows) {
+      tile.row[c] = (uint16_t)r;
+      atomicMax(&tile.n, c + 1);
     }
   }
-  if (tid == 0) sm.tile.adapter = a;
   __syncthreads();
   return true;
 }
 
-// t of one tile of rows: grid (tile, K range, 64 columns of t), MMA with the rows as A (M = 16) and the adapter's rows as B, both straight
-// from global memory: the sum over k may run in any order that both share, so a lane takes 16 contiguous bytes for two steps.  The
-// four warps take turns at 64 columns of k and meet in shared memory.
+// bf16 of a value, and what that loses (nothing where it is an infinity): 16 bits of the value in two halves.
+__device__ __forceinline__ void halves(float v, bf16& hi, bf16& lo) {
+  hi = __float2bfloat16_rn(v);
+  const float d = v - __bfloat162float(hi);
+  lo = __float2bfloat16_rn(fabsf(d) < INFINITY ? d : 0.f);
+}
+
+// t of one tile of rows: grid (tile, K range, 32 columns of t), a cluster holds the K ranges.  MMA with the rows as A (M = 16) and the
+// adapter's rows as B, both straight from global memory: the sum over k may run in any order that both share, so a lane takes 16
+// contiguous bytes for two steps.  The warps take turns at 64 columns of k and meet in shared memory, the ranges in that of the cluster's
+// first block; what leaves is scale * t as two bf16 halves (2^-17 of the adapter's share), the way adapter_up's MMA takes it.
 // Bound: latency for a few rows, the adapters' bytes for many tenants.
-constexpr int kDownCols = 64;
-__global__ void __launch_bounds__(kThreads) adapter_down_kernel(const AdapterArgs p) {
+constexpr int kDownCols = 32;
+constexpr int kMaxDownSplits = 8;
+__global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const AdapterArgs p) {
+  __shared__ union {
+    TileSmem find;
+    float red[kDownWarps][kTileRows][kDownCols + 2];
+  } sm;
+  __shared__ float part[kMaxDownSplits - 1][kTileRows * kDownCols];      // of the cluster's other blocks, in the first one
+  __shared__ RowTile tile;
+  __shared__ int leader;
+  const bool alone = p.splits == 1;
+  if (!alone) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ TileSmem sm;
-  __shared__ float red[kThreads / 32][kTileRows][kDownCols + 2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const bool any = find_tile(p, blockIdx.x, sm);
-  const int n = any ? sm.tile.n : 0;
-  if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) {
-    if (!any) sm.tile.adapter = -1;
-    p.tiles[blockIdx.x] = sm.tile;
-  }
-  if (!any || sm.tile.adapter < 0) return;
+  const bool any = find_tile(p, blockIdx.x, sm.find, tile, leader);
+  if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) p.tiles[blockIdx.x] = tile;
+  const int n = any && tile.adapter >= 0 ? tile.n : 0;               // the same in the whole cluster
   const int cols = p.n_seg * p.rank, col0 = blockIdx.z * kDownCols;
-  const int nt = min(kDownCols, cols - col0) / 8;
-  const int steps = (p.in + 63) / 64;
-  const int s0 = steps * (int)blockIdx.y / p.splits, s1 = steps * ((int)blockIdx.y + 1) / p.splits;
-  const bf16* x[2];
-  x[0] = g < n ? (const bf16*)p.x + (size_t)sm.tile.row[g] * p.in : nullptr;
-  x[1] = g + 8 < n ? (const bf16*)p.x + (size_t)sm.tile.row[g + 8] * p.in : nullptr;
-  const bf16* a = (const bf16*)p.a + ((size_t)sm.tile.adapter * cols + col0 + g) * p.in;
-  float acc[kDownCols / 8][4];
+  const int nt = min(kDownCols, cols - col0) / 8, width = nt * 8;
+  if (n > 0) {
+    const int steps = (p.in + 63) / 64;
+    const int s0 = steps * (int)blockIdx.y / p.splits, s1 = steps * ((int)blockIdx.y + 1) / p.splits;
+    const bf16* x[2];
+    x[0] = g < n ? (const bf16*)p.x + (size_t)tile.row[g] * p.in : nullptr;
+    x[1] = g + 8 < n ? (const bf16*)p.x + (size_t)tile.row[g + 8] * p.in : nullptr;
+    const bf16* a = (const bf16*)p.a + ((size_t)tile.adapter * cols + col0 + g) * p.in;
+    float acc[kDownCols / 8][4];
 #pragma unroll
-  for (int j = 0; j < kDownCols / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  for (int s = s0 + warp; s < s1; s += kThreads / 32) {
-    uint4 xv[2][2], av[kDownCols / 8][2];
+    for (int j = 0; j < kDownCols / 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 2
+    for (int s = s0 + warp; s < s1; s += kDownWarps) {
+      uint4 xv[2][2], av[kDownCols / 8][2];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int k = s * 64 + c * 32 + t * 8;
+      for (int c = 0; c < 2; ++c) {
+        const int k = s * 64 + c * 32 + t * 8;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) xv[i][c] = x[i] != nullptr && k < p.in ? *reinterpret_cast<const uint4*>(x[i] + k) : zero;
+        for (int i = 0; i < 2; ++i) xv[i][c] = x[i] != nullptr && k < p.in ? __ldg(reinterpret_cast<const uint4*>(x[i] + k)) : zero;
+#pragma unroll
+        for (int j = 0; j < kDownCols / 8; ++j)
+          av[j][c] = j < nt && k < p.in ? __ldg(reinterpret_cast<const uint4*>(a + (size_t)j * 8 * p.in + k)) : zero;
+      }
 #pragma unroll
       for (int j = 0; j < kDownCols / 8; ++j)
-        av[j][c] = j < nt && k < p.in ? *reinterpret_cast<const uint4*>(a + (size_t)j * 8 * p.in + k) : zero;
+        if (j < nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            mma_16816(acc[j], xv[0][c].x, xv[1][c].x, xv[0][c].y, xv[1][c].y, av[j][c].x, av[j][c].y);
+            mma_16816(acc[j], xv[0][c].z, xv[1][c].z, xv[0][c].w, xv[1][c].w, av[j][c].z, av[j][c].w);
+          }
     }
 #pragma unroll
     for (int j = 0; j < kDownCols / 8; ++j)
-      if (j < nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          mma_16816(acc[j], xv[0][c].x, xv[1][c].x, xv[0][c].y, xv[1][c].y, av[j][c].x, av[j][c].y);
-          mma_16816(acc[j], xv[0][c].z, xv[1][c].z, xv[0][c].w, xv[1][c].w, av[j][c].z, av[j][c].w);
-        }
+      if (j < nt) {
+        *reinterpret_cast<float2*>(&sm.red[warp][g][j * 8 + 2 * t]) = make_float2(acc[j][0], acc[j][1]);
+        *reinterpret_cast<float2*>(&sm.red[warp][g + 8][j * 8 + 2 * t]) = make_float2(acc[j][2], acc[j][3]);
+      }
   }
-#pragma unroll
-  for (int j = 0; j < kDownCols / 8; ++j)
-    if (j < nt) {
-      *reinterpret_cast<float2*>(&red[warp][g][j * 8 + 2 * t]) = make_float2(acc[j][0], acc[j][1]);
-      *reinterpret_cast<float2*>(&red[warp][g + 8][j * 8 + 2 * t]) = make_float2(acc[j][2], acc[j][3]);
-    }
   __syncthreads();
-  for (int i = tid; i < n * nt * 8; i += kThreads) {
-    const int r = i / (nt * 8), c = i - r * (nt * 8);
-    float v = red[0][r][c];
+  float mine[kTileRows * kDownCols / kDownThreads];
 #pragma unroll
-    for (int w = 1; w < kThreads / 32; ++w) v += red[w][r][c];
-    p.t[((size_t)blockIdx.y * p.rows + sm.tile.row[r]) * cols + col0 + c] = v;
+  for (int q = 0; q < kTileRows * kDownCols / kDownThreads; ++q) {
+    const int i = q * kDownThreads + tid, r = i / width, c = i - r * width;
+    mine[q] = 0.f;
+    if (i < n * width) {
+      mine[q] = sm.red[0][r][c];
+#pragma unroll
+      for (int w = 1; w < kDownWarps; ++w) mine[q] += sm.red[w][r][c];
+    }
+  }
+  if (!alone) {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // the first block has begun
+    if (blockIdx.y > 0) {
+#pragma unroll
+      for (int q = 0; q < kTileRows * kDownCols / kDownThreads; ++q) {
+        const int i = q * kDownThreads + tid;
+        if (i < n * width) {
+          uint32_t there;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&part[blockIdx.y - 1][i])));
+          asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(mine[q]) : "memory");
+        }
+      }
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blockIdx.y > 0) return;
+  }
+  if (n == 0) return;
+  const float scale = p.scale ? p.scale[tile.adapter] : 1.f;
+#pragma unroll
+  for (int q = 0; q < kTileRows * kDownCols / kDownThreads; ++q) {
+    const int i = q * kDownThreads + tid, r = i / width, c = i - r * width;
+    if (i < n * width) {
+      float v = mine[q];
+#pragma unroll
+      for (int k = 1; k < kMaxDownSplits; ++k)
+        if (k < p.splits) v += part[k - 1][i];
+      const size_t at = (size_t)tile.row[r] * cols + col0 + c;
+      halves(scale * v, p.t_hi[at], p.t_lo[at]);
+    }
   }
 }
 
@@ -231,30 +324,20 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// what rounding `v` to the bf16 in the upper half of `h` loses (nothing where that is an infinity)
-__device__ __forceinline__ float lost(float v, uint32_t h) {
-  const float d = v - __uint_as_float(h & 0xffff0000u);
-  return fabsf(d) < INFINITY ? d : 0.f;
-}
 __device__ __forceinline__ void add4(float4& a, const float4 v) { a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
-// four values from `left` on (all four where `vec`)
-__device__ __forceinline__ float4 get4(const float* p, int vec, int left) {
-  if (vec) return *reinterpret_cast<const float4*>(p);
-  float4 v = make_float4(p[0], 0.f, 0.f, 0.f);
-  if (left > 1) v.y = p[1];
-  if (left > 2) v.z = p[2];
-  if (left > 3) v.w = p[3];
-  return v;
+// four values, or the first `left` of them
+template <bool VEC>
+__device__ __forceinline__ float4 get4(const float* p, int left) {
+  if constexpr (VEC) return *reinterpret_cast<const float4*>(p);
+  return make_float4(p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
 }
-__device__ __forceinline__ void put4(float* p, float4 v, int vec, int left) {
-  if (vec) { *reinterpret_cast<float4*>(p) = v; return; }
-  p[0] = v.x;
-  if (left > 1) p[1] = v.y;
-  if (left > 2) p[2] = v.z;
-  if (left > 3) p[3] = v.w;
-}
-__device__ __forceinline__ void put4(bf16* p, float4 v, int vec, int left) {
-  if (vec) { *reinterpret_cast<uint2*>(p) = make_uint2(pack(v.x, v.y), pack(v.z, v.w)); return; }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put_all(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void put_all(bf16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack(v.x, v.y), pack(v.z, v.w)); }
+template <bool VEC, typename TY>
+__device__ __forceinline__ void put4(TY* p, float4 v, int left) {
+  if constexpr (VEC) { put_all(p, v); return; }
   put(p, v.x);
   if (left > 1) put(p + 1, v.y);
   if (left > 2) put(p + 2, v.z);
@@ -262,13 +345,17 @@ __device__ __forceinline__ void put4(bf16* p, float4 v, int vec, int left) {
 }
 
 // Reduction of the projection's partial sums, the adapters' way back up, one rounding: grid (columns, tile, segment), a warp has 16
-// columns of the tile's rows at a time.  MMA with t as A and b as B; t is split in two bf16 halves (16 bits of it, 2^-17 of the
-// adapter's share), its partial sums are added once per block.  A lane's two output tiles are numbered so that it owns four neighbouring
-// columns.  CHUNKS: 16 columns of t each.  Bound: L2 (partial sums) and the bytes of b and y.
-template <int CHUNKS, typename TY>
-__global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs p, const PartialView P, int steps, int vec) {
+// columns of the tile's rows at a time.  MMA with t's halves as A and b as B.  As in adapter_down the sum over j may run in any order: a
+// lane takes four (rank up to 16: QUADS = 0) or eight neighbouring j, QUADS is how many times 32 of them.  A lane's two output tiles are
+// numbered so that it owns four neighbouring columns.  A lane without a row reads row 0's sums, unconditionally (loads behind a branch are
+// waited for one by one: 7.4 us instead of 3.6 for one row of 4096), and writes nothing.  VEC: out is a multiple of four.  Bound: L2 (partial sums) and the bytes of b and y.
+__host__ __device__ constexpr int up_groups(int quads) { return quads <= 2 ? 2 : 1; }        // 16 columns each, whose loads are in flight together
+template <int QUADS, bool VEC, typename TY>
+__global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs p, const PartialView P, int steps) {
   pdl_wait();
   pdl_launch_dependents();
+  constexpr int CHUNKS = QUADS ? QUADS : 1, J = QUADS ? 8 : 4;           // j of a lane per chunk of 4 J
+  constexpr int GROUPS = up_groups(QUADS);
   const RowTile& tile = p.tiles[blockIdx.y];
   const int n = tile.n, adapter = tile.adapter, seg = blockIdx.z;
   if (n == 0) return;
@@ -277,63 +364,90 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
   int row[2];
   row[0] = g < n ? tile.row[g] : -1;
   row[1] = g + 8 < n ? tile.row[g + 8] : -1;
-  uint32_t hi[CHUNKS][4], lo[CHUNKS][4];
+  uint32_t hi[2][CHUNKS][J / 2], lo[2][CHUNKS][J / 2];                   // [row][chunk][pair of j]
+  auto load_j = [&](const bf16* src, bool there, uint32_t (&v)[J / 2]) {
+    if constexpr (J == 8) {
+      const uint4 u = there ? *reinterpret_cast<const uint4*>(src) : make_uint4(0u, 0u, 0u, 0u);
+      v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
+      const uint2 u = there ? *reinterpret_cast<const uint2*>(src) : make_uint2(0u, 0u);
+      v[0] = u.x; v[1] = u.y;
+    }
+  };
   if (adapter >= 0) {
-    const float scale = p.scale ? p.scale[adapter] : 1.f;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int j = c * 16 + t * 4;
-        if (row[i] >= 0 && j < p.rank) {
-          const float* src = p.t + (size_t)row[i] * cols + seg * p.rank + j;
-#pragma unroll 8
-          for (int s = 0; s < p.splits; ++s) add4(v, *reinterpret_cast<const float4*>(src + (size_t)s * p.rows * cols));
-        }
-        v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
-        const uint32_t h0 = pack(v.x, v.y), h1 = pack(v.z, v.w);
-        hi[c][i] = h0;
-        hi[c][2 + i] = h1;
-        lo[c][i] = pack(lost(v.x, h0 << 16), lost(v.y, h0));
-        lo[c][2 + i] = pack(lost(v.z, h1 << 16), lost(v.w, h1));
+        const int j = (c * 4 + t) * J;
+        const size_t at = (size_t)(row[i] < 0 ? 0 : row[i]) * cols + seg * p.rank + j;
+        load_j(p.t_hi + at, row[i] >= 0 && j < p.rank, hi[i][c]);
+        load_j(p.t_lo + at, row[i] >= 0 && j < p.rank, lo[i][c]);
       }
   }
   const bf16* b = (const bf16*)p.b + ((size_t)(adapter < 0 ? 0 : adapter) * p.n_seg + seg) * p.out * p.rank;
   for (int step = 0; step < steps; ++step) {
-    const int c0 = ((blockIdx.x * steps + step) * (kThreads / 32) + warp) * 16;
+    const int c0 = ((blockIdx.x * steps + step) * (kThreads / 32) + warp) * 16 * GROUPS;
     if (c0 >= p.out) return;
-    const int col = c0 + 4 * t, left = p.out - col;
-    float4 sum[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (row[i] >= 0 && left > 0) {
-        const float* src = P.p + (size_t)row[i] * P.ld + seg * p.out + col;
-#pragma unroll 8
-        for (int s = 0; s < P.splits; ++s) add4(sum[i], get4(src + s * P.split_stride, vec, left));
-      }
-    }
+    uint32_t bv[GROUPS][2][CHUNKS][J / 2];
     if (adapter >= 0) {
-      float acc[2][4];
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int o = c0 + q * 16 + 4 * (g >> 1) + 2 * i + (g & 1);
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c) {
+            const int j = (c * 4 + t) * J;
+            load_j(b + (size_t)o * p.rank + j, o < p.out && j < p.rank, bv[q][i][c]);
+          }
+        }
+    }
+    float4 sum[GROUPS][2];
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sum[q][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* src[GROUPS][2];
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-        const int o = c0 + 4 * (g >> 1) + 2 * i + (g & 1);
-        const bf16* src = b + (size_t)o * p.rank + t * 4;
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          const uint2 v = o < p.out && c * 16 + t * 4 < p.rank ? *reinterpret_cast<const uint2*>(src + c * 16) : make_uint2(0u, 0u);
-          mma_16816(acc[i], lo[c][0], lo[c][1], lo[c][2], lo[c][3], v.x, v.y);
-          mma_16816(acc[i], hi[c][0], hi[c][1], hi[c][2], hi[c][3], v.x, v.y);
-        }
+        const int col = c0 + q * 16 + 4 * t;
+        src[q][i] = P.p + (size_t)max(row[i], 0) * P.ld + seg * p.out + (col < p.out ? col : 0);
       }
-      add4(sum[0], make_float4(acc[0][0], acc[0][1], acc[1][0], acc[1][1]));
-      add4(sum[1], make_float4(acc[0][2], acc[0][3], acc[1][2], acc[1][3]));
+#pragma unroll 4
+    for (int s = 0; s < P.splits; ++s)
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) add4(sum[q][i], get4<VEC>(src[q][i] + s * P.split_stride, p.out - (c0 + q * 16 + 4 * t)));
+    if (adapter >= 0) {
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q) {
+        float acc[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int k = 0; k < J / 2; k += 2) {
+              mma_16816(acc[i], lo[0][c][k], lo[1][c][k], lo[0][c][k + 1], lo[1][c][k + 1], bv[q][i][c][k], bv[q][i][c][k + 1]);
+              mma_16816(acc[i], hi[0][c][k], hi[1][c][k], hi[0][c][k + 1], hi[1][c][k + 1], bv[q][i][c][k], bv[q][i][c][k + 1]);
+            }
+        }
+        add4(sum[q][0], make_float4(acc[0][0], acc[0][1], acc[1][0], acc[1][1]));
+        add4(sum[q][1], make_float4(acc[0][2], acc[0][3], acc[1][2], acc[1][3]));
+      }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (row[i] >= 0 && left > 0) put4((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + col, sum[i], vec, left);
+    for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int col = c0 + q * 16 + 4 * t;
+        if (row[i] >= 0 && col < p.out) put4<VEC>((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + col, sum[q][i], p.out - col);
+      }
   }
 }
 
@@ -354,12 +468,11 @@ int most_tiles(int rows, int n_adapters) {
   const int64_t n = (int64_t)n_adapters + 1 + rows / kTileRows;
   return n < rows ? (int)n : rows;
 }
-constexpr int kMaxDownSplits = 16;
-// K ranges of adapter_down: about two blocks per SM, 64 columns of k for each warp at least
+// K ranges of adapter_down, a cluster: about two blocks per SM, 64 columns of k for each warp at least
 int down_splits(int in, int blocks) {
-  const int most = (in + 255) / 256, want = (296 + blocks - 1) / blocks;
-  const int s = want < most ? want : most;
-  return s > kMaxDownSplits ? kMaxDownSplits : s;
+  int s = 1;
+  while (s < kMaxDownSplits && s * kDownWarps * 64 < in && s * blocks < 296) s *= 2;
+  return s;
 }
 size_t tiles_bytes(int rows) { return round256(sizeof(RowTile) * rows); }
 
@@ -370,20 +483,41 @@ amph_status bad_shape(int n_seg, int out, int rows, int rank) {
     return api_fail(AMPH_ERR_SHAPE, "rank must be a multiple of 8 in 8..%d (got %d)", AMPH_MAX_ADAPTER_RANK, rank);
   return AMPH_OK;
 }
-size_t t_bytes(int n_seg, int rows, int rank) { return round256((size_t)kMaxDownSplits * rows * n_seg * rank * sizeof(float)); }
+size_t t_bytes(int n_seg, int rows, int rank) { return round256((size_t)rows * n_seg * rank * sizeof(float)); }
 
+template <int QUADS, typename TY>
+cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaStream_t st) {
+  // a warp's columns: 16 or 32, or several times as many where that still leaves several blocks per SM
+  const int cols = kThreads / 32 * 16 * up_groups(QUADS), blocks = (p.out + cols - 1) / cols;
+  int steps = (int)((int64_t)blocks * tiles * p.n_seg / (148 * 8));
+  steps = steps < 1 ? 1 : (steps > 4 ? 4 : steps);
+  const dim3 grid((blocks + steps - 1) / steps, tiles, p.n_seg);
+  return p.out % 4 == 0 ? launch_pdl(adapter_up_kernel<QUADS, true, TY>, grid, dim3(kThreads), 0, st, p, pv, steps)
+                        : launch_pdl(adapter_up_kernel<QUADS, false, TY>, grid, dim3(kThreads), 0, st, p, pv, steps);
+}
 template <typename TY>
 cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaStream_t st) {
-  // a block's columns: 64, or more where that still leaves several blocks per SM
-  const int groups = (p.out + 63) / 64;
-  int steps = (int)((int64_t)groups * tiles * p.n_seg / (148 * 8));
-  steps = steps < 1 ? 1 : (steps > 4 ? 4 : steps);
-  const dim3 grid((groups + steps - 1) / steps, tiles, p.n_seg);
-  const int vec = p.out % 4 == 0;
-  if (p.rank <= 16) return launch_pdl(adapter_up_kernel<1, TY>, grid, dim3(kThreads), 0, st, p, pv, steps, vec);
-  if (p.rank <= 32) return launch_pdl(adapter_up_kernel<2, TY>, grid, dim3(kThreads), 0, st, p, pv, steps, vec);
-  if (p.rank <= 64) return launch_pdl(adapter_up_kernel<4, TY>, grid, dim3(kThreads), 0, st, p, pv, steps, vec);
-  return launch_pdl(adapter_up_kernel<8, TY>, grid, dim3(kThreads), 0, st, p, pv, steps, vec);
+  if (p.rank <= 16) return run_up<0, TY>(p, pv, tiles, st);
+  if (p.rank <= 32) return run_up<1, TY>(p, pv, tiles, st);
+  if (p.rank <= 64) return run_up<2, TY>(p, pv, tiles, st);
+  return run_up<4, TY>(p, pv, tiles, st);
+}
+
+cudaError_t run_down(const AdapterArgs& p, int tiles, int col_blocks, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(tiles, p.splits, col_blocks);
+  cfg.blockDim = dim3(kDownThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 1;
+  at[1].val.clusterDim.y = p.splits;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, adapter_down_kernel, p);
 }
 
 amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* const* w, int32_t n_seg, int32_t out, int32_t in,
@@ -413,6 +547,8 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   p.row_adapter = row_adapter;
   p.tiles = (RowTile*)ws_dev;
   p.t = (float*)((char*)ws_dev + tiles_bytes(rows));
+  p.t_hi = (bf16*)p.t;
+  p.t_lo = p.t_hi + (size_t)rows * cols;
   p.y = y_dev;
   p.status = status_dev;
   p.n_adapters = ad->n_adapters; p.rank = ad->rank; p.n_seg = n_seg; p.out = out; p.in = in; p.rows = rows; p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks);
@@ -450,7 +586,7 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   if (dtype == AMPH_DTYPE_F32)
     e = launch_pdl(adapter_down_plain_kernel, dim3((cols + 3) / 4, rows), dim3(kThreads), 0, st, p);
   else
-    e = launch_pdl(adapter_down_kernel, dim3(tiles, p.splits, col_blocks), dim3(kThreads), 0, st, p);
+    e = run_down(p, tiles, col_blocks, st);
   if (e == cudaSuccess) {
     if (g) {
       int splits = 0;
