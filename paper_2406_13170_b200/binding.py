@@ -434,6 +434,24 @@ def _want(t: torch.Tensor, name: str, device: torch.device, dtype, shape=None) -
     return t
 
 
+_stream_scratch: Dict[tuple, torch.Tensor] = {}
+
+
+def _scratch(kind: str, index: int, stream: int, need: int, device: torch.device):
+    """(scratch of at least `need` bytes for a call on this stream of the current device, whether it is one that was zero at first and
+    only calls of this kind have used).
+
+    Calls on one stream follow one another, so a stream keeps one piece per kind.  A call that is captured into a graph gets a piece
+    of its own from the graph's memory: graphs may be replayed beside one another and beside anything else."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(need, dtype=torch.uint8, device=device), False
+    key = (kind, index, stream)
+    t = _stream_scratch.get(key)
+    if t is None or t.numel() < need:
+        t = _stream_scratch[key] = torch.zeros(need, dtype=torch.uint8, device=device)
+    return t, True
+
+
 class Adapters:
     """Low-rank adapters of a projection with n_seg weight matrices (amph_adapters).
 
@@ -526,13 +544,14 @@ def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use
     L = lib()
     out, in_ = adapters.w_shape
     if y is None:
-        y = torch.empty((rows, n_seg * out), dtype=y_dtype or dt, device=adapters.device)
+        y = x.new_empty((rows, n_seg * out)) if y_dtype is None else x.new_empty((rows, n_seg * out), dtype=y_dtype)
     need = adapters.scratch_bytes(rows)
-    scratch = torch.empty(need, dtype=torch.uint8, device=adapters.device)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    scratch = _scratch("adapters", index, stream, need, adapters.device)[0]
     arr = adapters.w_array(*[w.data_ptr() for w in ws])
     rc = L.amph_project_adapters(x.data_ptr(), x.shape[0], arr, n_seg, out, in_, rows, _DTYPES[dt], int(use_tensor_core), adapters.ref,
                                  row_adapter.data_ptr(), y.data_ptr(), _DTYPES[y.dtype], scratch.data_ptr(), need,
-                                 None if status is None else status.data_ptr(), torch._C._cuda_getCurrentRawStream(index))
+                                 None if status is None else status.data_ptr(), stream)
     if rc != 0:
         raise AmphError(rc, L.amph_last_error(None).decode())
     return y
@@ -623,17 +642,13 @@ def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v
     return q_out
 
 
-_attention_scratch: Dict[tuple, torch.Tensor] = {}      # (device, stream) -> scratch whose counters are zero between calls
-
-
 def paged_attention(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, scale: float = 0.0,
                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                     status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """amph_paged_attention: one new token of every sequence, q [n_seqs, n_heads, head_dim], against positions 0 .. lens - 1 of its
     pages.  lens int32 [n_seqs]; lse fp32 [n_seqs, n_heads] receives the logarithm of the softmax's sums; scale 0: 1 / sqrt(head_dim).
 
-    The scratch belongs to the stream that the call runs on: one piece per stream, kept; a call that is captured into a
-    graph has its own, from the graph's memory."""
+    Scratch: see _scratch."""
     index, dt = cache.index, cache.dtype
     if torch.cuda.current_device() != index:
         with torch.cuda.device(index):
@@ -659,15 +674,10 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, len
     if status is not None:
         _want(status, "status", cache.device, torch.int32)
     stream = torch._C._cuda_getCurrentRawStream(index)
-    if torch.cuda.is_current_stream_capturing():
-        scratch, clean = torch.empty(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=cache.device), 0
-    else:
-        scratch, clean = _attention_scratch.get((index, stream)), 1
-        if scratch is None:
-            scratch = _attention_scratch[(index, stream)] = torch.zeros(AMPH_PAGED_WS_BYTES, dtype=torch.uint8, device=cache.device)
+    scratch, clean = _scratch("attention", index, stream, AMPH_PAGED_WS_BYTES, cache.device)
     L = lib()
     rc = L.amph_paged_attention(cache.ref, q.data_ptr(), heads, lens.data_ptr(), table.data_ptr(), n, table.shape[1], scale, out.data_ptr(),
-                                None if lse is None else lse.data_ptr(), scratch.data_ptr(), AMPH_PAGED_WS_BYTES, clean,
+                                None if lse is None else lse.data_ptr(), scratch.data_ptr(), AMPH_PAGED_WS_BYTES, int(clean),
                                 None if status is None else status.data_ptr(), stream)
     if rc != 0:
         raise AmphError(rc, L.amph_last_error(None).decode())

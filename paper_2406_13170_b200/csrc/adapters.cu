@@ -468,10 +468,10 @@ int most_tiles(int rows, int n_adapters) {
   const int64_t n = (int64_t)n_adapters + 1 + rows / kTileRows;
   return n < rows ? (int)n : rows;
 }
-// K ranges of adapter_down, a cluster: about two blocks per SM, 64 columns of k for each warp at least
+// K ranges of adapter_down, a cluster: as many blocks as run at a time (three per SM), 64 columns of k for each warp at least
 int down_splits(int in, int blocks) {
   int s = 1;
-  while (s < kMaxDownSplits && s * kDownWarps * 64 < in && s * blocks < 296) s *= 2;
+  while (s < kMaxDownSplits && s * kDownWarps * 64 < in && 2 * s * blocks <= 444) s *= 2;
   return s;
 }
 size_t tiles_bytes(int rows) { return round256(sizeof(RowTile) * rows); }
