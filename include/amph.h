@@ -359,7 +359,7 @@ amph_status amph_project_adapters(const void* x_dev, int32_t x_rows_cap, const v
                                   const int32_t* row_adapter, void* y_dev, int32_t y_dtype, void* ws_dev, size_t ws_bytes,
                                   int32_t* status_dev, void* stream);
 
-/* One layer's paged cache: k_pages and v_pages [n_pages][n_kv_heads][page_size][head_dim] of dtype, device, 16-byte aligned.
+/* One layer's paged cache: k_pages and v_pages [n_pages][n_kv_heads][page_size][head_dim] of dtype, device, 32-byte aligned.
  * head_dim 64 or 128; page_size a power of two, at most 65536.  A page table (device int32 [n_seqs][table_stride]) names the
  * pages of every sequence in order: position p of sequence s is slot p % page_size of page table[s][p / page_size].  Entries
  * behind a sequence's last page are not read.  Sequences may share pages that no call writes. */

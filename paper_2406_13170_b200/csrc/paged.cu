@@ -10,10 +10,6 @@ namespace {
 
 typedef __nv_bfloat16 bf16;
 
-template <typename T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
-
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
@@ -290,10 +286,13 @@ struct PlainItem {
   }
 };
 
-__device__ __forceinline__ uint4 load_once(const bf16* p) {          // 16 bytes that no other thread of the block reads
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+// 32 or 16 bytes that no other thread of the block reads
+__device__ __forceinline__ void load_once(const bf16* p, uint32_t (&v)[8]) {
+  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
+}
+__device__ __forceinline__ void load_once(const bf16* p, uint32_t (&v)[4]) {
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "l"(p));
 }
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -307,34 +306,34 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
 // Keys [k0, k1) of one bf16 item on the warp-level tensor cores, 16 keys of a warp at a time, straight from the pages to registers:
 // no shared memory, no barrier, the next 16 keys' loads in flight while these are worked on.
 //   Scores   S[head][key]: A = queries (rows 0-7; rows 8-15 zero), B = keys.  The sum over head_dim may run in any order that both
-//            operands share, so a lane takes 16 contiguous bytes of its key for two steps.
+//            operands share, so a lane takes 32 contiguous bytes of its key for four steps.
 //   Values   O[head][column]: A = weights, B = values.  Rows 8-15 carry what the weights of rows 0-7 lose when they are rounded to
-//            bf16, so 16 bits of every weight enter at no further cost; columns may be numbered in any order, so a lane takes 16
-//            contiguous bytes of four keys and pairs them with byte permutes.
+//            bf16, so 16 bits of every weight enter at no further cost; columns may be numbered in any order, so a lane takes
+//            head_dim / 8 contiguous ones of four keys and pairs them with byte permutes.
 // Bound: HBM.  A key's 4 head_dim bytes cost at most 16 head_dim * 4 flops, a tenth of what the tensor pipe does meanwhile.
 template <int DH>
 struct MmaItem {
   struct Smem {};
   static __device__ __forceinline__ void run(const AttendParams& p, Smem&, MergeSmem<DH>& out, int seq, int kv, int head0, int heads, int k0, int k1) {
-    constexpr int C = DH / 32, H = DH / 64;
+    constexpr int C = DH / 64, W = DH / 16;          // 128-byte parts of a key; 32-bit words of a value row that a lane takes
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const bf16* kp = (const bf16*)p.k;
     const bf16* vp = (const bf16*)p.v;
     const bool wide = p.page_shift >= 4;             // 16 keys share a page
     const int page_mask = (1 << p.page_shift) - 1;
-    uint4 q[C];
+    uint32_t q[C][8];
 #pragma unroll
-    for (int c = 0; c < C; ++c) q[c] = make_uint4(0u, 0u, 0u, 0u);
-    if (g < heads) {
-      const bf16* qp = (const bf16*)p.q + ((int64_t)seq * p.n_heads + head0 + g) * DH + t * 8;
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int c = 0; c < C; ++c) q[c] = *reinterpret_cast<const uint4*>(qp + c * 32);
-    }
-    float o[H][8][4];
+      for (int i = 0; i < 8; i += 4) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (g < heads)
+          v = *reinterpret_cast<const uint4*>((const bf16*)p.q + ((int64_t)seq * p.n_heads + head0 + g) * DH + c * 64 + t * 16 + i * 2);
+        q[c][i] = v.x; q[c][i + 1] = v.y; q[c][i + 2] = v.z; q[c][i + 3] = v.w;
+      }
+    float o[2 * W][4];
 #pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[h][j][0] = o[h][j][1] = o[h][j][2] = o[h][j][3] = 0.f;
+    for (int j = 0; j < 2 * W; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
 
     // lane j (and j + 16) knows the page of key j of the 16 at `key0`; -1: none
@@ -347,23 +346,34 @@ struct MmaItem {
       const int from = __shfl_sync(~0u, page, wide ? 0 : j);
       return ((((int64_t)from * p.n_kv + kv) << p.page_shift) + ((key0 + j) & page_mask)) * DH;
     };
-    uint4 kr[2][C], vr[4][H];
+    uint32_t kr[2][C][8], vr[4][W];
     auto load_k = [&](int key0, int page, unsigned there) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const int j = n * 8 + g;
-        const bf16* src = kp + row_of(key0, page, j) + t * 8;
+        const bf16* src = kp + row_of(key0, page, j) + t * 16;
 #pragma unroll
-        for (int c = 0; c < C; ++c) kr[n][c] = (there >> j) & 1 ? load_once(src + c * 32) : make_uint4(0u, 0u, 0u, 0u);
+        for (int c = 0; c < C; ++c) {
+          if ((there >> j) & 1) {
+            load_once(src + c * 64, kr[n][c]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) kr[n][c][i] = 0u;
+          }
+        }
       }
     };
     auto load_v = [&](int key0, int page, unsigned there) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int j = 2 * t + (i & 1) + (i >> 1) * 8;
-        const bf16* src = vp + row_of(key0, page, j) + g * 8;
+        const bf16* src = vp + row_of(key0, page, j) + g * 2 * W;
+        if ((there >> j) & 1) {
+          load_once(src, vr[i]);
+        } else {
 #pragma unroll
-        for (int h = 0; h < H; ++h) vr[i][h] = (there >> j) & 1 ? load_once(src + h * 64) : make_uint4(0u, 0u, 0u, 0u);
+          for (int w = 0; w < W; ++w) vr[i][w] = 0u;
+        }
       }
     };
     int key0 = k0 + warp * 16;
@@ -378,10 +388,9 @@ struct MmaItem {
       for (int n = 0; n < 2; ++n) {
         s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          mma_16816(s[n], q[c].x, 0u, q[c].y, 0u, kr[n][c].x, kr[n][c].y);
-          mma_16816(s[n], q[c].z, 0u, q[c].w, 0u, kr[n][c].z, kr[n][c].w);
-        }
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) mma_16816(s[n], q[c][i], 0u, q[c][i + 1], 0u, kr[n][c][i], kr[n][c][i + 1]);
       }
       const unsigned now = there;
       there = __ballot_sync(~0u, page_next >= 0);
@@ -401,11 +410,9 @@ struct MmaItem {
         const float alpha = weight(m_run, mx);
         l_run *= alpha;
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+        for (int j = 0; j < 2 * W; ++j)
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[h][j][i] *= alpha;
+          for (int i = 0; i < 4; ++i) o[j][i] *= alpha;
         m_run = mx;
       }
       uint32_t hi[2], lo[2];
@@ -418,14 +425,9 @@ struct MmaItem {
         lo[n] = pack(w[n][0] - __uint_as_float(hi[n] << 16), w[n][1] - __uint_as_float(hi[n] & 0xffff0000u));
       }
 #pragma unroll
-      for (int h = 0; h < H; ++h) {
-        const uint32_t v[4][4] = {{vr[0][h].x, vr[0][h].y, vr[0][h].z, vr[0][h].w}, {vr[1][h].x, vr[1][h].y, vr[1][h].z, vr[1][h].w},
-                                  {vr[2][h].x, vr[2][h].y, vr[2][h].z, vr[2][h].w}, {vr[3][h].x, vr[3][h].y, vr[3][h].z, vr[3][h].w}};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t pick = j & 1 ? 0x7632u : 0x5410u;
-          mma_16816(o[h][j], hi[0], lo[0], hi[1], lo[1], __byte_perm(v[0][j >> 1], v[1][j >> 1], pick), __byte_perm(v[2][j >> 1], v[3][j >> 1], pick));
-        }
+      for (int j = 0; j < 2 * W; ++j) {
+        const uint32_t pick = j & 1 ? 0x7632u : 0x5410u;
+        mma_16816(o[j], hi[0], lo[0], hi[1], lo[1], __byte_perm(vr[0][j >> 1], vr[1][j >> 1], pick), __byte_perm(vr[2][j >> 1], vr[3][j >> 1], pick));
       }
       load_v(key0 + kUnit, page_next, there);
       page_next = find(key0 + 2 * kUnit);
@@ -434,14 +436,11 @@ struct MmaItem {
     l_run += __shfl_xor_sync(~0u, l_run, 2);
     if (g < heads) {
 #pragma unroll
-      for (int h = 0; h < H; ++h)
+      for (int j = 0; j < 2 * W; j += 4)
 #pragma unroll
-        for (int j = 0; j < 8; j += 4)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<float4*>(&out.o[warp][g][h * 64 + t * 16 + i * 8 + j]) =
-                make_float4(o[h][j][i] + o[h][j][i + 2], o[h][j + 1][i] + o[h][j + 1][i + 2], o[h][j + 2][i] + o[h][j + 2][i + 2],
-                            o[h][j + 3][i] + o[h][j + 3][i + 2]);
+        for (int i = 0; i < 2; ++i)                   // columns 2 W n + j of n = 2 t + i
+          *reinterpret_cast<float4*>(&out.o[warp][g][2 * W * (2 * t + i) + j]) =
+              make_float4(o[j][i] + o[j][i + 2], o[j + 1][i] + o[j + 1][i + 2], o[j + 2][i] + o[j + 2][i + 2], o[j + 3][i] + o[j + 3][i + 2]);
       if (t == 0) {
         out.m[warp][g] = m_run;
         out.l[warp][g] = l_run;
@@ -454,11 +453,53 @@ struct MmaItem {
 // The block that holds unit u when `total` units are spread over n blocks (block c begins at total * c / n).
 __device__ __forceinline__ int block_of(long long u, long long total, int n) { return (int)(((u + 1) * n - 1) / total); }
 
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack(v.x, v.y), pack(v.z, v.w)); }
+
+// Sums of one (or more) sets of weights that share the maximum m: sum of w V in o, sum of w in l.
+struct Sums {
+  float4 o;
+  float m, l;
+};
+__device__ __forceinline__ void add_scaled(Sums& a, float f, float4 o, float l) {
+  a.o.x += f * o.x; a.o.y += f * o.y; a.o.z += f * o.z; a.o.w += f * o.w;
+  a.l += f * l;
+}
 template <typename T, int DH>
-__device__ __forceinline__ void write_row(const AttendParams& p, int seq, int head, int col, float o, float m, float l) {
+__device__ __forceinline__ void write_row(const AttendParams& p, int seq, int head, int col, const Sums& a) {
   const int64_t at = (int64_t)seq * p.n_heads + head;
-  ((T*)p.out)[at * DH + col] = from_f<T>(l == 0.f ? 0.f : o / l);     // l = 0: no key at all
-  if (p.lse != nullptr && col == 0) p.lse[at] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) / kLog2e + logf(l);
+  const float4 o = a.l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.o.x / a.l, a.o.y / a.l, a.o.z / a.l, a.o.w / a.l);   // l = 0: no key at all
+  store4((T*)p.out + at * DH + col, o);
+  if (p.lse != nullptr && col == 0) p.lse[at] = a.l == 0.f ? -INFINITY : (a.m == -INFINITY ? 0.f : a.m) / kLog2e + logf(a.l);
+}
+
+// Columns 4 i .. 4 i + 3 of an item (i counts over its heads) from parts first, first + step, ... below `count` of those in `all`.  Eight
+// parts' loads are in flight at a time; the parts are added in their order.
+__device__ __noinline__ Sums add_parts(const float* all, int part_floats, int dh, int i, int first, int step, int count) {
+  Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+  const int ml_at = kHeads * dh + 2 * (4 * i / dh);
+  for (int c = first; c < count; c += 8 * step) {
+    float4 o[8];
+    float2 ml[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int k = min(c + q * step, count - 1);
+      const float* x = all + (size_t)(2 * k + (k == 0)) * part_floats;      // the first block's part 1, part 0 behind it
+      ml[q] = __ldcg(reinterpret_cast<const float2*>(x + ml_at));
+      o[q] = __ldcg(reinterpret_cast<const float4*>(x) + i);
+    }
+    float m = a.m;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (c + q * step < count) m = fmaxf(m, ml[q].x);
+    const Sums old = a;
+    a = {make_float4(0.f, 0.f, 0.f, 0.f), m, 0.f};
+    if (c != first) add_scaled(a, weight(old.m, m), old.o, old.l);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (c + q * step < count) add_scaled(a, weight(ml[q].x, m), o[q], ml[q].y);
+  }
+  return a;
 }
 
 template <typename T, int DH, typename Item>
@@ -469,7 +510,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
   __shared__ typename Item::Smem sm;
   __shared__ long long s_sum[kAttWarps], s_before;
   __shared__ int s_seq, s_last;
-  __shared__ float s_m[kHeads], s_l[kHeads];
+  __shared__ float2 s_ml[kAttThreads];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int items = p.n_kv * p.head_blocks;
 
@@ -502,7 +543,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
   // sequences without keys
   for (int s = blockIdx.x; s < p.n_seqs; s += gridDim.x)
     if (clamped_len(p, s) == 0)
-      for (int i = tid; i < p.n_heads * DH; i += kAttThreads) write_row<T, DH>(p, s, i / DH, i % DH, 0.f, 0.f, 0.f);
+      for (int i = tid; i < p.n_heads * DH / 4; i += kAttThreads) write_row<T, DH>(p, s, 4 * i / DH, 4 * i % DH, Sums{});
 
   const int n = (int)(total < gridDim.x ? total : gridDim.x);
   if ((int)blockIdx.x >= n) return;
@@ -532,23 +573,20 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
     const bool whole = take == tiles;
     const long long first = u - tile;
     float* part = p.parts + ((size_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * p.part_floats;
-    for (int i = tid; i < heads * DH; i += kAttThreads) {
-      const int h = i / DH, c = i % DH;
-      float m = mg.m[0][h];
+    const int slots = heads * DH / 4;
+    for (int i = tid; i < slots; i += kAttThreads) {
+      const int h = 4 * i / DH, c = 4 * i % DH;
+      Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), mg.m[0][h], 0.f};
 #pragma unroll
-      for (int w = 1; w < kAttWarps; ++w) m = fmaxf(m, mg.m[w][h]);
-      float o = 0.f, l = 0.f;
+      for (int w = 1; w < kAttWarps; ++w) a.m = fmaxf(a.m, mg.m[w][h]);
 #pragma unroll
-      for (int w = 0; w < kAttWarps; ++w) {
-        const float f = weight(mg.m[w][h], m);
-        o += f * mg.o[w][h][c];
-        l += f * mg.l[w][h];
-      }
+      for (int w = 0; w < kAttWarps; ++w)
+        add_scaled(a, weight(mg.m[w][h], a.m), *reinterpret_cast<const float4*>(&mg.o[w][h][c]), mg.l[w][h]);
       if (whole) {
-        write_row<T, DH>(p, seq, head0 + h, c, o, m, l);
+        write_row<T, DH>(p, seq, head0 + h, c, a);
       } else {
-        part[i] = o;
-        if (c == 0) { part[kHeads * DH + 2 * h] = m; part[kHeads * DH + 2 * h + 1] = l; }
+        reinterpret_cast<float4*>(part)[i] = a.o;
+        if (c == 0) *reinterpret_cast<float2*>(part + kHeads * DH + 2 * h) = make_float2(a.m, a.l);
       }
     }
     if (!whole) {
@@ -562,33 +600,30 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
       __syncthreads();
       if (s_last) {
         __threadfence();
-        const float* all = p.parts + (size_t)c0 * 2 * p.part_floats;       // block c0 + i: part 1 for i = 0, part 0 behind it
-        for (int h = warp; h < heads; h += kAttWarps) {
-          float m = -INFINITY;
-          for (int c = lane; c <= c1 - c0; c += 32)
-            m = fmaxf(m, __ldcg(all + (size_t)(2 * c + (c == 0)) * p.part_floats + kHeads * DH + 2 * h));
-#pragma unroll
-          for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-          float l = 0.f;
-          for (int c = lane; c <= c1 - c0; c += 32) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(all + (size_t)(2 * c + (c == 0)) * p.part_floats + kHeads * DH + 2 * h));
-            l += ml.y * weight(ml.x, m);
+        const float* all = p.parts + (size_t)c0 * 2 * p.part_floats;
+        const int count = c1 - c0 + 1;
+        if (2 * slots <= kAttThreads) {           // few columns: several groups of threads share the parts
+          const int groups = kAttThreads / slots, group = tid / slots, i = tid - group * slots;
+          Sums a = {};
+          if (group < groups) {
+            a = add_parts(all, p.part_floats, DH, i, group, groups, count);
+            reinterpret_cast<float4*>(mg.o)[tid] = a.o;
+            s_ml[tid] = make_float2(a.m, a.l);
           }
-#pragma unroll
-          for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(~0u, l, d);
-          if (lane == 0) { s_m[h] = m; s_l[h] = l; }
-        }
-        __syncthreads();
-        for (int i = tid; i < heads * DH; i += kAttThreads) {
-          const int h = i / DH;
-          const float m = s_m[h];
-          float o = 0.f;
-#pragma unroll 8
-          for (int c = 0; c <= c1 - c0; ++c) {
-            const float* x = all + (size_t)(2 * c + (c == 0)) * p.part_floats;
-            o += __ldcg(x + i) * weight(__ldcg(x + kHeads * DH + 2 * h), m);
+          __syncthreads();
+          if (group == 0) {
+            float m = a.m;
+            for (int k = 1; k < groups; ++k) m = fmaxf(m, s_ml[k * slots + i].x);
+            Sums all_groups = {make_float4(0.f, 0.f, 0.f, 0.f), m, 0.f};
+            for (int k = 0; k < groups; ++k) {
+              const float2 ml = s_ml[k * slots + i];
+              add_scaled(all_groups, weight(ml.x, m), reinterpret_cast<const float4*>(mg.o)[k * slots + i], ml.y);
+            }
+            write_row<T, DH>(p, seq, head0 + 4 * i / DH, 4 * i % DH, all_groups);
           }
-          write_row<T, DH>(p, seq, head0 + h, i % DH, o, m, s_l[h]);
+        } else {
+          for (int i = tid; i < slots; i += kAttThreads)
+            write_row<T, DH>(p, seq, head0 + 4 * i / DH, 4 * i % DH, add_parts(all, p.part_floats, DH, i, 0, 1, count));
         }
       }
     }
@@ -620,7 +655,7 @@ amph_status check_cache(const amph_paged_cache* c, int32_t n_seqs, int32_t table
   if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
     return api_fail(AMPH_ERR_SHAPE, "page_size must be a power of two, at most 65536 (got %d)", c->page_size);
   if (n_seqs < 0 || table_stride < 1) return api_fail(AMPH_ERR_SHAPE, "n_seqs must not be negative and table_stride positive");
-  if (!aligned16(c->k_pages) || !aligned16(c->v_pages)) return api_fail(AMPH_ERR_INVALID_ARG, "the pages must be 16-byte aligned");
+  if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages) & 31) return api_fail(AMPH_ERR_INVALID_ARG, "the pages must be 32-byte aligned");
   *shift = 0;
   while ((1 << *shift) < c->page_size) ++*shift;
   return AMPH_OK;

@@ -45,6 +45,11 @@ def test_attention_and_write_refuse_caches(L, fault, status):
     assert _message(L)
 
 
+def test_pages_that_32_byte_loads_cannot_take(L):
+    for fault in (dict(k_pages=P + 16), dict(v_pages=P + 16)):
+        assert _attend(L, _cache(**fault)) == 1 and "32-byte" in _message(L)
+
+
 @pytest.mark.parametrize("fault,status", [
     (dict(q=None), 1), (dict(lens=None), 1), (dict(table=None), 1), (dict(out=None), 1), (dict(out=P), 1), (dict(q=P + 2), 1),
     (dict(n_heads=0), 2), (dict(n_heads=6), 2), (dict(n_heads=2048), 2), (dict(n_seqs=-1), 2), (dict(n_seqs=4097), 2), (dict(stride=0), 2),
