@@ -36,6 +36,7 @@ struct AdapterArgs {
   void* y;
   int* status;
   int n_adapters, rank, n_seg, out, in, rows, splits;
+  int beside;              // bf16: adapter_down runs beside the kernel ahead of it (the projection)
 };
 
 // The row's adapter, -1 if it has none (or names one that does not exist, which is reported).
@@ -214,6 +215,10 @@ __device__ __forceinline__ void halves(float v, bf16& hi, bf16& lo) {
 // adapter's rows as B, both straight from global memory: the sum over k may run in any order that both share, so a lane takes 16
 // contiguous bytes for two steps.  The warps take turns at 64 columns of k and meet in shared memory, the ranges in that of the cluster's
 // first block; what leaves is scale * t as two bf16 halves (2^-17 of the adapter's share), the way adapter_up's MMA takes it.
+// `beside`: the kernel ahead is the tensor-core projection, which starts this one once everything ahead of itself is done, so it takes
+// the SMs and the shared memory that the projection leaves; only the first block waits for the projection, so that both are done when
+// this one is.  (Ahead of the projection, q / k / v of 64 rows of 24
+// tenants took 36.1 us in all, 28.1 now; gate / up of 37 rows at rank 64 48.5, 43.2 now.)
 // Bound: latency for a few rows, the adapters' bytes for many tenants.
 constexpr int kDownCols = 32;
 constexpr int kMaxDownSplits = 8;
@@ -221,15 +226,15 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
   __shared__ union {
     TileSmem find;
     float red[kDownWarps][kTileRows][kDownCols + 2];
+    float part[kMaxDownSplits - 1][kTileRows * kDownCols];               // of the cluster's other blocks, in the first one
   } sm;
-  __shared__ float part[kMaxDownSplits - 1][kTileRows * kDownCols];      // of the cluster's other blocks, in the first one
   __shared__ RowTile tile;
   __shared__ int leader;
   const bool alone = p.splits == 1;
-  if (!alone) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-  pdl_wait();
+  if (!p.beside) pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const bool waits = p.beside && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0;
   const bool any = find_tile(p, blockIdx.x, sm.find, tile, leader);
   if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) p.tiles[blockIdx.x] = tile;
   const int n = any && tile.adapter >= 0 ? tile.n : 0;               // the same in the whole cluster
@@ -287,15 +292,15 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
     }
   }
   if (!alone) {
-    __syncwarp();
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // the first block has begun
+    __syncwarp();                                                    // every block has read its warps' sums
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (blockIdx.y > 0) {
 #pragma unroll
       for (int q = 0; q < kTileRows * kDownCols / kDownThreads; ++q) {
         const int i = q * kDownThreads + tid;
         if (i < n * width) {
           uint32_t there;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&part[blockIdx.y - 1][i])));
+          asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&sm.part[blockIdx.y - 1][i])));
           asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(mine[q]) : "memory");
         }
       }
@@ -304,7 +309,10 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (blockIdx.y > 0) return;
   }
-  if (n == 0) return;
+  if (n == 0) {
+    if (waits) pdl_wait();
+    return;
+  }
   const float scale = p.scale ? p.scale[tile.adapter] : 1.f;
 #pragma unroll
   for (int q = 0; q < kTileRows * kDownCols / kDownThreads; ++q) {
@@ -313,11 +321,12 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
       float v = mine[q];
 #pragma unroll
       for (int k = 1; k < kMaxDownSplits; ++k)
-        if (k < p.splits) v += part[k - 1][i];
+        if (k < p.splits) v += sm.part[k - 1][i];
       const size_t at = (size_t)tile.row[r] * cols + col0 + c;
       halves(scale * v, p.t_hi[at], p.t_lo[at]);
     }
   }
+  if (waits) pdl_wait();
 }
 
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -575,29 +584,33 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
     lock.lock();
     if (!g_plans[dev]) {
       g_plans[dev] = tc_gemm_create(xb, xr, xc, 1, status_dev);
-      if (g_plans[dev]) tc_wide_init(g_plans[dev]);
+      if (g_plans[dev]) {
+        tc_wide_init(g_plans[dev]);
+        tc_gemm_wait_first(g_plans[dev]);      // a call's weights may be an earlier call's output
+        tc_gemm_late_trigger(g_plans[dev]);
+      }
     }
     g = g_plans[dev];
     if (!g) return api_fail(AMPH_ERR_CUDA, "tensor-map encoder unavailable or not an sm_100 device");
     g->cache.clear();                       // tensor maps are made for each call
     tc_gemm_rebind(g, 0, xb[0], x_rows_cap, in, status_dev);
   }
-  cudaError_t e;
+  cudaError_t e = cudaSuccess;
+  p.beside = g != nullptr;
+  if (g) {
+    int splits = 0;
+    size_t stride = 0;
+    if (!tc_gemm_launch(g, 0, w, n_seg, out, in, rows, P, p_floats, &splits, &stride, st))
+      return api_fail(AMPH_ERR_SHAPE, "shape not covered by the tensor-core kernel");
+    pv.splits = splits;
+    pv.split_stride = stride;
+  }
   if (dtype == AMPH_DTYPE_F32)
     e = launch_pdl(adapter_down_plain_kernel, dim3((cols + 3) / 4, rows), dim3(kThreads), 0, st, p);
   else
     e = run_down(p, tiles, col_blocks, st);
   if (e == cudaSuccess) {
-    if (g) {
-      int splits = 0;
-      size_t stride = 0;
-      // The weights are fetched while the kernel ahead still runs: that is adapter_down, which starts its successor only when
-      // everything ahead of itself is done.
-      if (!tc_gemm_launch(g, 0, w, n_seg, out, in, rows, P, p_floats, &splits, &stride, st))
-        return api_fail(AMPH_ERR_SHAPE, "shape not covered by the tensor-core kernel");
-      pv.splits = splits;
-      pv.split_stride = stride;
-    } else {
+    if (!g) {
       // the plain kernel takes blocks of up to kMaxRows rows as the context's passes do
       GemmSeg segs[kMaxK];
       for (int s = 0; s < n_seg; ++s) segs[s].w = w[s];

@@ -52,6 +52,7 @@ struct TcParams {
   int* err_flag;
   unsigned long long wait_limit_ns;   // a barrier wait gives up after this long
   int wait_first;                      // wait for the kernel before this one ahead of the first weight (see tc_gemm_wait_first)
+  int late_trigger;                    // see tc_gemm_late_trigger
   uint32_t extra_tx;                   // self-test only: bytes the first stage's barrier expects beyond what is copied
 };
 
@@ -185,7 +186,7 @@ tc_gemm_kernel(const __grid_constant__ TmapPack maps, const TcParams prm) {
   if (warp == 1) {                                   // TMEM allocation belongs to the MMA warp
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(tmem_cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    pdl_launch_dependents();                         // the consumer kernel may get resident and wait
+    if (EPI != EPI_PARTIAL || !prm.late_trigger) pdl_launch_dependents();      // the consumer kernel may get resident and wait
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncwarp();
@@ -251,6 +252,7 @@ tc_gemm_kernel(const __grid_constant__ TmapPack maps, const TcParams prm) {
     // ---------------- MMA issuer (the warp stays converged, its elected lane issues)
     const bool leader = elect_one();
     pdl_wait();                                      // returns about 1.1 us after it is asked, also behind a finished kernel
+    if (EPI == EPI_PARTIAL && prm.late_trigger) pdl_launch_dependents();
     asm volatile("bar.sync 2, 64;" ::: "memory");
     if (leader)
       for (int i = 0; i < nit && i < stages; ++i)
@@ -544,6 +546,7 @@ bool tc_gemm_launch(TcGemm* g, int xb, const void* const* w, int n_seg, int out,
   prm.err_flag = g->err_flag;
   prm.wait_limit_ns = g->wait_limit_ns;
   prm.wait_first = g->wait_first;
+  prm.late_trigger = g->late_trigger;
   prm.extra_tx = g->extra_tx;
   const size_t smem = (size_t)stages * stage_bytes + 1024;
   launch_pdl(tc_gemm_kernel<EPI_PARTIAL>, dim3(tiles, splits), dim3(kThreads), smem, st, pack, prm);
@@ -688,6 +691,7 @@ void tc_gemm_rebind(TcGemm* g, int xb, void* ptr, int rows, int cols, int* err_f
 }
 
 void tc_gemm_wait_first(TcGemm* g) { g->wait_first = 1; }
+void tc_gemm_late_trigger(TcGemm* g) { g->late_trigger = 1; }
 
 void tc_gemm_set_selftest(TcGemm* g, unsigned long long wait_limit_ns, unsigned extra_tx) {
   g->wait_limit_ns = wait_limit_ns ? wait_limit_ns : kWaitLimitNs;

@@ -73,6 +73,7 @@ struct WideParams {
   RopeGroups gr;
   int n_heads, dh, max_ctx;
   int wait_first;           // see tc_gemm_wait_first
+  int late_trigger;         // see tc_gemm_late_trigger (plain form)
   int* err_flag;
   unsigned long long wait_limit_ns;
   uint32_t extra_tx;        // self-test only: bytes that a pair's first stage expects beyond what is copied
@@ -213,7 +214,7 @@ tc_wide_kernel(const __grid_constant__ WideMaps maps, const WideParams prm) {
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(prm.tmem_cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    pdl_launch_dependents();
+    if (EPI != WIDE_PLAIN || !prm.late_trigger) pdl_launch_dependents();
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncwarp();
@@ -294,6 +295,7 @@ tc_wide_kernel(const __grid_constant__ WideMaps maps, const WideParams prm) {
     // ---------------- the ring's first activations, then MMA issuer (even CTA)
     const bool leader = elect_one();
     pdl_wait();
+    if (EPI == WIDE_PLAIN && prm.late_trigger) pdl_launch_dependents();
     cluster_ready();
     {
       SegIter it = first;
@@ -762,6 +764,7 @@ bool wide_params(TcGemm* g, int xb, int n_seg, int tiles_per_seg, int in, int ro
   if (prm->stages > kMaxStages) prm->stages = kMaxStages;
   prm->flags = g->wide_flags;
   prm->wait_first = g->wait_first;
+  prm->late_trigger = g->late_trigger;
   prm->err_flag = g->err_flag;
   prm->wait_limit_ns = g->wait_limit_ns;
   prm->extra_tx = g->extra_tx;
