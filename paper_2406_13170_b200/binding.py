@@ -412,7 +412,7 @@ def project_noalloc(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use_
 
 # ---------------------------------------------------------------------------------------------------------------------
 # Operators for decoding many requests over one set of weights.  They run on torch's current stream of the tensors' device, never
-# synchronise, and return tensors whose contents are there in stream order.
+# synchronise, and return tensors whose contents are there in stream order.  Scratch is kept per stream (csrc/torch_ops.cpp).
 # ---------------------------------------------------------------------------------------------------------------------
 _DTYPES = {torch.float32: AMPH_DTYPE_F32, torch.bfloat16: AMPH_DTYPE_BF16}
 
@@ -434,22 +434,26 @@ def _want(t: torch.Tensor, name: str, device: torch.device, dtype, shape=None) -
     return t
 
 
-_stream_scratch: Dict[tuple, torch.Tensor] = {}
+_torch_ops = None
 
 
-def _scratch(kind: str, index: int, stream: int, need: int, device: torch.device):
-    """(scratch of at least `need` bytes for a call on this stream of the current device, whether it is one that was zero at first and
-    only calls of this kind have used).
+def _ops():
+    """The native way from tensors to the library's operators (csrc/torch_ops.cpp, built beside libamph.so)."""
+    global _torch_ops
+    if _torch_ops is None:
+        try:
+            from . import torch_ops
+        except ModuleNotFoundError as e:
+            raise FileNotFoundError("torch_ops.so is missing: run `python -m paper_2406_13170_b200.build`") from e
+        torch_ops.load(lib()._handle)
+        _torch_ops = torch_ops
+    return _torch_ops
 
-    Calls on one stream follow one another, so a stream keeps one piece per kind.  A call that is captured into a graph gets a piece
-    of its own from the graph's memory: graphs may be replayed beside one another and beside anything else."""
-    if torch.cuda.is_current_stream_capturing():
-        return torch.empty(need, dtype=torch.uint8, device=device), False
-    key = (kind, index, stream)
-    t = _stream_scratch.get(key)
-    if t is None or t.numel() < need:
-        t = _stream_scratch[key] = torch.zeros(need, dtype=torch.uint8, device=device)
-    return t, True
+
+def _failed(rc) -> None:
+    if rc is NotImplemented:
+        _refuse(1, "these arguments do not fit together")
+    raise AmphError(rc, lib().amph_last_error(None).decode())
 
 
 class Adapters:
@@ -475,23 +479,8 @@ class Adapters:
         if scale is not None:
             _want(scale, "scale", a.device, torch.float32, (self.n,))
         self.tensors = (a, b, scale)
-        self.index = a.device.index
-        self.w_shape = (self.out, self.in_)
-        self.w_array = C.c_void_p * self.n_seg
         self.c = amph_adapters(a.data_ptr(), b.data_ptr(), None if scale is None else scale.data_ptr(), self.n, self.rank)
-        self.ref = C.byref(self.c)
-        self._bytes: Dict[int, int] = {}
-
-    def scratch_bytes(self, rows: int) -> int:
-        """amph_project_adapters_bytes for this many rows."""
-        need = self._bytes.get(rows)
-        if need is None:
-            L, n = lib(), C.c_size_t()
-            rc = L.amph_project_adapters_bytes(self.n_seg, self.out, rows, self.rank, C.byref(n))
-            if rc != 0:
-                raise AmphError(rc, L.amph_last_error(None).decode())
-            need = self._bytes[rows] = n.value
-        return need
+        self.handle = _ops().adapters(C.addressof(self.c), self.n_seg, self.out, self.in_, _DTYPES[self.dtype], a.device.index)
 
 
 def _check_adapters_call(x, ws, rows, adapters, row_adapter, y, y_dtype, status):
@@ -529,32 +518,12 @@ def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use
     """amph_project_adapters: y[r] = x[r] . W^T + scale (x[r] . a^T) . b^T with the adapter row_adapter[r] (int32 [rows], < 0: none).
 
     x, ws, rows, use_tensor_core as for `project`; y [rows, n_seg * out] of y_dtype (default: x's type)."""
-    n_seg, index, dt = adapters.n_seg, adapters.index, adapters.dtype
-    ok = (len(ws) == n_seg and x.dim() == 2 and x.dtype is dt and x.get_device() == index and x.is_contiguous()
-          and row_adapter.dtype is torch.int32 and row_adapter.get_device() == index and row_adapter.shape == (rows,)
-          and row_adapter.is_contiguous() and x.shape[1] == adapters.in_ and y is None and y_dtype is None and status is None)
-    if ok:
-        for w in ws:
-            ok = ok and w.dtype is dt and w.get_device() == index and w.shape == adapters.w_shape and w.is_contiguous()
-    if not ok:
-        _check_adapters_call(x, ws, rows, adapters, row_adapter, y, y_dtype, status)
-    if torch.cuda.current_device() != index:
-        with torch.cuda.device(index):
-            return project_adapters(x, ws, rows, use_tensor_core, adapters, row_adapter, y, y_dtype, status)
-    L = lib()
-    out, in_ = adapters.w_shape
-    if y is None:
-        y = x.new_empty((rows, n_seg * out)) if y_dtype is None else x.new_empty((rows, n_seg * out), dtype=y_dtype)
-    need = adapters.scratch_bytes(rows)
-    stream = torch._C._cuda_getCurrentRawStream(index)
-    scratch = _scratch("adapters", index, stream, need, adapters.device)[0]
-    arr = adapters.w_array(*[w.data_ptr() for w in ws])
-    rc = L.amph_project_adapters(x.data_ptr(), x.shape[0], arr, n_seg, out, in_, rows, _DTYPES[dt], int(use_tensor_core), adapters.ref,
-                                 row_adapter.data_ptr(), y.data_ptr(), _DTYPES[y.dtype], scratch.data_ptr(), need,
-                                 None if status is None else status.data_ptr(), stream)
-    if rc != 0:
-        raise AmphError(rc, L.amph_last_error(None).decode())
-    return y
+    r = (_torch_ops or _ops()).project_adapters(adapters.handle, x, ws, rows, use_tensor_core, row_adapter, y, y_dtype, status)
+    if type(r) is int or r is NotImplemented:
+        if r is NotImplemented:
+            _check_adapters_call(x, ws, rows, adapters, row_adapter, y, y_dtype, status)
+        _failed(r)
+    return r
 
 
 class PagedCache:
@@ -573,8 +542,7 @@ class PagedCache:
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
         self.c = amph_paged_cache(k_pages.data_ptr(), v_pages.data_ptr(), _DTYPES[self.dtype], self.n_kv_heads, self.head_dim,
                                   self.page_size, self.n_pages)
-        self.ref = C.byref(self.c)
-        self.index = self.device.index
+        self.handle = _ops().cache(C.addressof(self.c), self.device.index)
 
     def _table(self, table: torch.Tensor) -> None:
         if table.dim() != 2:
@@ -582,19 +550,38 @@ class PagedCache:
         _want(table, "table", self.device, torch.int32)
 
 
-def _rows_of(t: torch.Tensor, name: str, cache: PagedCache, rows: int, heads: int, dtype) -> int:
-    """Checks [rows, heads * head_dim] or [rows, heads, head_dim] whose rows are contiguous; returns the row stride in elements."""
+def _rows_of(t: torch.Tensor, name: str, cache: PagedCache, rows: int, heads: int, dtype) -> None:
+    """Checks [rows, heads * head_dim] or [rows, heads, head_dim] whose rows are contiguous."""
     dh = cache.head_dim
     stride = t.stride()
     if len(stride) == 2:
         fits = t.shape == (rows, heads * dh) and stride[1] == 1
     else:
         fits = t.shape == (rows, heads, dh) and stride[2] == 1 and (stride[1] == dh or heads == 1)
-    if t.dtype is not dtype or t.get_device() != cache.index:
+    if t.dtype is not dtype or t.device != cache.device:
         _refuse(1, f"{name} must be {dtype} on {cache.device} (got {t.dtype} on {t.device})")
     if not fits:
         _refuse(2, f"{name} must be {rows} rows of {heads} heads of {dh}, each row contiguous (got {tuple(t.shape)}, strides {stride})")
-    return stride[0] if rows > 1 else heads * dh
+
+
+def _check_write_call(cache, q, k, v, row_seq, row_pos, table, q_out, status):
+    if k.dtype not in _DTYPES or k.dim() < 2:
+        _refuse(2, f"k must be float32 or bfloat16 rows (got {k.dtype}, {tuple(k.shape)})")
+    rows, dt = k.shape[0], k.dtype
+    _rows_of(k, "k", cache, rows, cache.n_kv_heads, dt)
+    _rows_of(v, "v", cache, rows, cache.n_kv_heads, dt)
+    if q is not None:
+        heads = (q.shape[1] * q.shape[2] if q.dim() == 3 else q.shape[-1]) // cache.head_dim
+        _rows_of(q, "q", cache, rows, heads, dt)
+        if q_out is not None:
+            _want(q_out, "q_out", cache.device, cache.dtype, (rows, heads, cache.head_dim))
+    elif q_out is not None:
+        _refuse(1, "q_out without q")
+    _want(row_seq, "row_seq", cache.device, torch.int32, (rows,))
+    _want(row_pos, "row_pos", cache.device, torch.int32, (rows,))
+    cache._table(table)
+    if status is not None:
+        _want(status, "status", cache.device, torch.int32)
 
 
 def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, row_seq: torch.Tensor,
@@ -604,81 +591,39 @@ def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v
 
     q [rows, n_heads * head_dim] (or None), k, v [rows, n_kv_heads * head_dim], fp32 or bf16 (one type), each row contiguous (slices
     of a projection's output); row_seq, row_pos int32 [rows], row_seq < 0: the row is skipped (its place in a new q_out is not set)."""
-    index, rows, dt = cache.index, k.shape[0], k.dtype
-    if dt not in _DTYPES:
-        _refuse(2, f"k must be float32 or bfloat16 (got {dt})")
-    if torch.cuda.current_device() != index:
-        with torch.cuda.device(index):
-            return paged_write(cache, q, k, v, row_seq, row_pos, table, theta, q_out, status)
-    ks = _rows_of(k, "k", cache, rows, cache.n_kv_heads, dt)
-    vs = _rows_of(v, "v", cache, rows, cache.n_kv_heads, dt)
-    heads = qs = 0
-    if q is not None:
-        heads = (q.shape[1] * q.shape[2] if q.dim() == 3 else q.shape[-1]) // cache.head_dim
-        qs = _rows_of(q, "q", cache, rows, heads, dt)
-        if q_out is None:
-            q_out = torch.empty(rows, heads, cache.head_dim, dtype=cache.dtype, device=cache.device)
-        elif not (q_out.dtype is cache.dtype and q_out.get_device() == index and q_out.shape == (rows, heads, cache.head_dim) and q_out.is_contiguous()):
-            _want(q_out, "q_out", cache.device, cache.dtype, (rows, heads, cache.head_dim))
-    elif q_out is not None:
-        _refuse(1, "q_out without q")
-    shape = (rows,)
-    if not (row_seq.dtype is torch.int32 and row_pos.dtype is torch.int32 and table.dtype is torch.int32 and row_seq.shape == shape
-            and row_pos.shape == shape and table.dim() == 2 and row_seq.get_device() == index and row_pos.get_device() == index
-            and table.get_device() == index and row_seq.is_contiguous() and row_pos.is_contiguous() and table.is_contiguous()):
-        _want(row_seq, "row_seq", cache.device, torch.int32, shape)
-        _want(row_pos, "row_pos", cache.device, torch.int32, shape)
-        cache._table(table)
+    r = (_torch_ops or _ops()).paged_write(cache.handle, q, k, v, row_seq, row_pos, table, theta, q_out, status)
+    if type(r) is int or r is NotImplemented:
+        if r is NotImplemented:
+            _check_write_call(cache, q, k, v, row_seq, row_pos, table, q_out, status)
+        _failed(r)
+    return r
+
+
+def _check_attention_call(cache, q, table, lens, out, lse, status):
+    if q.dim() != 3:
+        _refuse(2, f"q must be [n_seqs, n_heads, head_dim] (got {tuple(q.shape)})")
+    n, heads = q.shape[:2]
+    _want(q, "q", cache.device, cache.dtype, (n, heads, cache.head_dim))
+    cache._table(table)
+    if table.shape[0] != n:
+        _refuse(2, f"table has {table.shape[0]} rows for {n} sequences")
+    _want(lens, "lens", cache.device, torch.int32, (n,))
+    if out is not None:
+        _want(out, "out", cache.device, cache.dtype, q.shape)
+    if lse is not None:
+        _want(lse, "lse", cache.device, torch.float32, (n, heads))
     if status is not None:
         _want(status, "status", cache.device, torch.int32)
-    L = lib()
-    n_seqs, width = table.shape
-    rc = L.amph_paged_write(cache.ref, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[dt], heads, rows,
-                            row_seq.data_ptr(), row_pos.data_ptr(), table.data_ptr(), n_seqs, width, theta,
-                            None if q is None else q_out.data_ptr(), None if status is None else status.data_ptr(),
-                            torch._C._cuda_getCurrentRawStream(index))
-    if rc != 0:
-        raise AmphError(rc, L.amph_last_error(None).decode())
-    return q_out
 
 
 def paged_attention(cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, scale: float = 0.0,
                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                     status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """amph_paged_attention: one new token of every sequence, q [n_seqs, n_heads, head_dim], against positions 0 .. lens - 1 of its
-    pages.  lens int32 [n_seqs]; lse fp32 [n_seqs, n_heads] receives the logarithm of the softmax's sums; scale 0: 1 / sqrt(head_dim).
-
-    Scratch: see _scratch."""
-    index, dt = cache.index, cache.dtype
-    if torch.cuda.current_device() != index:
-        with torch.cuda.device(index):
-            return paged_attention(cache, q, table, lens, scale, out, lse, status)
-    shape = q.shape
-    n, heads = (shape[0], shape[1]) if len(shape) == 3 else (0, 0)
-    if not (len(shape) == 3 and shape[2] == cache.head_dim and q.dtype is dt and lens.dtype is torch.int32 and table.dtype is torch.int32
-            and lens.shape == (n,) and table.dim() == 2 and table.shape[0] == n and q.get_device() == index and lens.get_device() == index
-            and table.get_device() == index and q.is_contiguous() and lens.is_contiguous() and table.is_contiguous()):
-        if len(shape) != 3:
-            _refuse(2, f"q must be [n_seqs, n_heads, head_dim] (got {tuple(shape)})")
-        _want(q, "q", cache.device, dt, (n, heads, cache.head_dim))
-        cache._table(table)
-        if table.shape[0] != n:
-            _refuse(2, f"table has {table.shape[0]} rows for {n} sequences")
-        _want(lens, "lens", cache.device, torch.int32, (n,))
-    if out is None:
-        out = torch.empty_like(q)
-    else:
-        _want(out, "out", cache.device, dt, shape)
-    if lse is not None:
-        _want(lse, "lse", cache.device, torch.float32, (n, heads))
-    if status is not None:
-        _want(status, "status", cache.device, torch.int32)
-    stream = torch._C._cuda_getCurrentRawStream(index)
-    scratch, clean = _scratch("attention", index, stream, AMPH_PAGED_WS_BYTES, cache.device)
-    L = lib()
-    rc = L.amph_paged_attention(cache.ref, q.data_ptr(), heads, lens.data_ptr(), table.data_ptr(), n, table.shape[1], scale, out.data_ptr(),
-                                None if lse is None else lse.data_ptr(), scratch.data_ptr(), AMPH_PAGED_WS_BYTES, int(clean),
-                                None if status is None else status.data_ptr(), stream)
-    if rc != 0:
-        raise AmphError(rc, L.amph_last_error(None).decode())
-    return out
+    pages.  lens int32 [n_seqs]; lse fp32 [n_seqs, n_heads] receives the logarithm of the softmax's sums; scale 0: 1 / sqrt(head_dim)."""
+    r = (_torch_ops or _ops()).paged_attention(cache.handle, q, table, lens, scale, out, lse, status)
+    if type(r) is int or r is NotImplemented:
+        if r is NotImplemented:
+            _check_attention_call(cache, q, table, lens, out, lse, status)
+        _failed(r)
+    return r
