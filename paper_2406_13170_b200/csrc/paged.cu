@@ -10,13 +10,24 @@ namespace {
 
 typedef __nv_bfloat16 bf16;
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+// eight values as they lie in memory, and as fp32
+template <typename T> struct Raw8 { uint4 u[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  return r;
 }
-__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ void values(const Raw8<float>& r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[4 * i] = __uint_as_float(r.u[i].x); v[4 * i + 1] = __uint_as_float(r.u[i].y);
+    v[4 * i + 2] = __uint_as_float(r.u[i].z); v[4 * i + 3] = __uint_as_float(r.u[i].w);
+  }
+}
+__device__ __forceinline__ void values(const Raw8<bf16>& r, float (&v)[8]) {
+  const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = __uint_as_float(w[i] << 16);
@@ -40,7 +51,7 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
 // ---------------------------------------------------------------------------------------------------------------------
 // amph_paged_write
 // ---------------------------------------------------------------------------------------------------------------------
-constexpr int kWriteThreads = 256;
+constexpr int kWriteThreads = 256;       // at most
 
 struct WriteParams {
   const void *q, *k, *v;
@@ -65,15 +76,29 @@ __device__ __forceinline__ float2 cos_sin_of_phase(u64 phase) {
   return make_float2(c, s);
 }
 
-// Grid (row, part of the row's heads); a thread takes eight rotation pairs of one head at a time (eight values twice for v).
-// Bound: HBM for many rows, latency for few: the rows' loads do not depend on the table's, and several parts share a row.
-template <typename TS, typename TD>
+// Grid (row, part of the row's heads); an item is eight rotation pairs of one head (eight values twice for v), a thread has ITEMS, whose
+// loads are under way while the row's place in the cache is looked up.  Bound: HBM for many rows, latency for few (see run_write).
+template <typename TS, typename TD, int ITEMS>
 __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid_constant__ WriteParams p) {
   pdl_wait();
   pdl_launch_dependents();
   __shared__ float2 cs[64];
   const int row = blockIdx.x, half = p.dh >> 1;
   const int seq = p.row_seq[row], pos = p.row_pos[row];
+  const int per_head = half >> 3, shift = p.dh == 128 ? 3 : 2;
+  const int items = (p.n_heads + 2 * p.n_kv) * per_head, item0 = blockIdx.y * ITEMS * blockDim.x + threadIdx.x;
+  Raw8<TS> lo[ITEMS], hi[ITEMS];
+#pragma unroll
+  for (int n = 0; n < ITEMS; ++n) {
+    const int it = item0 + n * blockDim.x;
+    if (it >= items) break;
+    const int head = it >> shift, i = (it & (per_head - 1)) * 8, hk = head - p.n_heads;
+    const TS* src = head < p.n_heads ? (const TS*)p.q + row * p.q_stride + head * p.dh
+                    : hk < p.n_kv    ? (const TS*)p.k + row * p.k_stride + hk * p.dh
+                                     : (const TS*)p.v + row * p.v_stride + (hk - p.n_kv) * p.dh;
+    lo[n] = load8(src + i);
+    hi[n] = load8(src + half + i);
+  }
   if (seq < 0) return;
   bool ok = seq < p.n_seqs && pos >= 0 && (pos >> p.page_shift) < p.table_stride;
   int page = 0;
@@ -85,34 +110,26 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid
     if (p.status != nullptr && threadIdx.x == 0) *p.status = AMPH_ERR_INVALID_ARG;
     return;
   }
-  if (threadIdx.x < half) cs[threadIdx.x] = cos_sin_of_phase((u64)pos * p.turn[threadIdx.x]);
+  for (int i = threadIdx.x; i < half; i += blockDim.x) cs[i] = cos_sin_of_phase((u64)pos * p.turn[i]);
   __syncthreads();
-  const int per_head = half >> 3;
-  const int items = (p.n_heads + 2 * p.n_kv) * per_head;
   const int64_t slot = pos & ((1 << p.page_shift) - 1);
-  for (int it = blockIdx.y * kWriteThreads + threadIdx.x; it < items; it += gridDim.y * kWriteThreads) {
-    const int head = it / per_head, i = (it - head * per_head) * 8;
-    const TS* src;
-    TD* dst;
-    if (head < p.n_heads) {
-      src = (const TS*)p.q + row * p.q_stride + head * p.dh;
-      dst = (TD*)p.q_out + ((int64_t)row * p.n_heads + head) * p.dh;
-    } else {
-      const int h = head - p.n_heads, is_v = h >= p.n_kv, hk = is_v ? h - p.n_kv : h;
-      src = is_v ? (const TS*)p.v + row * p.v_stride : (const TS*)p.k + row * p.k_stride;
-      src += hk * p.dh;
-      dst = (TD*)(is_v ? p.v_pages : p.k_pages) + ((((int64_t)page * p.n_kv + hk) << p.page_shift) + slot) * p.dh;
-    }
+#pragma unroll
+  for (int n = 0; n < ITEMS; ++n) {
+    const int it = item0 + n * blockDim.x;
+    if (it >= items) break;
+    const int head = it >> shift, i = (it & (per_head - 1)) * 8, h = head - p.n_heads, is_v = h >= p.n_kv, hk = is_v ? h - p.n_kv : h;
+    TD* dst = head < p.n_heads ? (TD*)p.q_out + ((int64_t)row * p.n_heads + head) * p.dh
+                               : (TD*)(is_v ? p.v_pages : p.k_pages) + ((((int64_t)page * p.n_kv + hk) << p.page_shift) + slot) * p.dh;
     float a[8], b[8];
-    load8(src + i, a);
-    load8(src + half + i, b);
-    if (head < p.n_heads + p.n_kv) {
+    values(lo[n], a);
+    values(hi[n], b);
+    if (h < p.n_kv) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float2 t = cs[i + j];
-        const float lo = a[j] * t.x - b[j] * t.y;
+        const float x = a[j] * t.x - b[j] * t.y;
         b[j] = b[j] * t.x + a[j] * t.y;
-        a[j] = lo;
+        a[j] = x;
       }
     }
     store8(dst + i, a);
@@ -683,10 +700,19 @@ void fill_turns(float theta, int dh, u64* turn) {
   memcpy(turn, kept.turn, sizeof(u64) * (dh / 2));
 }
 
+// One item a thread while all blocks run at once (8 rows of 32 heads: 2.4 us, 2.9 with three), three beyond (8,000 rows of 32 / 8 heads in
+// bf16: 30.0 us, 5.6 TB/s; 34.7 with one or two, 31.5 with four).
+template <typename TS, typename TD, int ITEMS>
+cudaError_t run_write_items(const WriteParams& p, int rows, int items, cudaStream_t st) {
+  // blocks of one row's parts, all of the same size
+  const int parts = (items + ITEMS * kWriteThreads - 1) / (ITEMS * kWriteThreads);
+  const int threads = ((items + parts * ITEMS - 1) / (parts * ITEMS) + 31) / 32 * 32;
+  return launch_pdl(paged_write_kernel<TS, TD, ITEMS>, dim3(rows, parts), dim3(threads), 0, st, p);
+}
 template <typename TS, typename TD>
 cudaError_t run_write(const WriteParams& p, int rows, cudaStream_t st) {
   const int items = (p.n_heads + 2 * p.n_kv) * (p.dh / 16);
-  return launch_pdl(paged_write_kernel<TS, TD>, dim3(rows, (items + 2 * kWriteThreads - 1) / (2 * kWriteThreads)), dim3(kWriteThreads), 0, st, p);
+  return (int64_t)rows * items <= 148 * 4 * kWriteThreads ? run_write_items<TS, TD, 1>(p, rows, items, st) : run_write_items<TS, TD, 3>(p, rows, items, st);
 }
 
 template <typename T, int DH, typename Item>

@@ -316,6 +316,15 @@ def test_write(heads, kv, dh, page, seqs, source, dtype, theta):
         assert torch.equal(now, before)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("source", [torch.bfloat16, torch.float32], ids=["from_bf16", "from_fp32"])
+@pytest.mark.parametrize("heads,kv,dh,page,seqs", [
+    (32, 8, 128, 16, [(0, 333), (70001, 90)]), (5, 1, 64, 32, [(7, 5500)]), (33, 3, 128, 64, [(0, 517)]), (0, 2, 64, 1, [(0, 9500)]),
+])
+def test_write_of_many_rows(heads, kv, dh, page, seqs, source, dtype):
+    test_write(heads, kv, dh, page, seqs, source, dtype, 10000.0)
+
+
 def test_angles_of_far_positions():
     """Position 2^31 - 2^16: the angle's phase is exact, cosine and sine are those of 64-bit arithmetic on an exact product."""
     from paper_2406_13170_b200 import PagedCache, paged_write
