@@ -391,7 +391,7 @@ amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64
  * ws_clean = 0 the call clears them itself (scratch with any contents), with ws_clean = 1 the caller vouches for them (cleared
  * once, used by these calls alone).  Calls that may overlap on the GPU need scratch of their own.  Equal inputs give equal bits. */
 #define AMPH_PAGED_MAX_SEQS 4096
-#define AMPH_PAGED_WS_COUNTERS 4096u
+#define AMPH_PAGED_WS_COUNTERS 8192u
 #define AMPH_PAGED_WS_BYTES (5u << 20)
 amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, int32_t n_heads, const int32_t* lens,
                                  const int32_t* table, int32_t n_seqs, int32_t table_stride, float scale, void* out, float* lse,

@@ -31,7 +31,7 @@ EXPORTS = ["amph_workspace_bytes", "amph_init", "amph_load_weights", "amph_prefi
            "amph_reset", "amph_destroy", "amph_last_error"]
 AMPH_MAX_ADAPTER_RANK = 128
 AMPH_PAGED_MAX_SEQS = 4096
-AMPH_PAGED_WS_COUNTERS = 4096
+AMPH_PAGED_WS_COUNTERS = 8192
 AMPH_PAGED_WS_BYTES = 5 << 20
 
 

@@ -141,11 +141,12 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid
 // amph_paged_attention
 //
 // The work is a line of units of kUnit keys: sequence by sequence, in a sequence item by item (a key / value head and up to kHeads of
-// the query heads that share it), in an item unit by unit.  The grid is as many blocks as the device runs at a time, and
+// the query heads that share it), in an item unit by unit, with one unit more ahead of each item for what an item costs whatever its length
+// (the pipeline fills, the warps' sums are joined).  The grid is as many blocks as the device runs at a time, and
 // block c takes units [total * c / n, total * (c + 1) / n): every length mix is spread evenly, and the host needs no length.  An item
 // inside one block is finished there.  Of an item cut over blocks each leaves its part (running maximum, sum, weighted values)
-// in scratch, and the block that arrives last adds the parts in the order of the blocks: no block waits, and the
-// bits do not depend on who is last.  Statistics and sums are fp32.
+// in scratch.  Of every kGroup neighbouring parts the block that arrives last adds them in the order of the blocks, and of the groups the
+// one that is done last adds those: no block waits, and the bits do not depend on who is last.  Statistics and sums are fp32.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kUnit = 64;                // keys: 16 for each warp
 constexpr int kAttWarps = 4;
@@ -153,6 +154,7 @@ constexpr int kAttThreads = kAttWarps * 32;
 constexpr int kAttResident = 3;          // blocks per SM: 168 registers a thread
 constexpr int kHeads = 8;                // query heads of an item
 constexpr int kMaxBlocks = 592;
+constexpr int kGroup = 8;                // parts that one block adds at a time: as many as it has loads in flight
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct AttendParams {
@@ -160,7 +162,7 @@ struct AttendParams {
   const int *lens, *table;
   void* out;
   float* lse;
-  int* counters;           // [kMaxBlocks]: parts that arrived of the item that begins in block c and goes on behind it
+  int* counters;           // [2][kMaxBlocks]: parts that arrived of the group that begins in block c | groups of the item that begins there
   float* parts;            // [kMaxBlocks][2][part_floats]: block c's part of an item that began before it | begins in it
   int* status;
   int part_floats;
@@ -467,9 +469,6 @@ struct MmaItem {
   }
 };
 
-// The block that holds unit u when `total` units are spread over n blocks (block c begins at total * c / n).
-__device__ __forceinline__ int block_of(long long u, long long total, int n) { return (int)(((u + 1) * n - 1) / total); }
-
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack(v.x, v.y), pack(v.z, v.w)); }
 
@@ -490,34 +489,49 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int seq, int he
   if (p.lse != nullptr && col == 0) p.lse[at] = a.l == 0.f ? -INFINITY : (a.m == -INFINITY ? 0.f : a.m) / kLog2e + logf(a.l);
 }
 
-// Columns 4 i .. 4 i + 3 of an item (i counts over its heads) from parts first, first + step, ... below `count` of those in `all`.  Eight
-// parts' loads are in flight at a time; the parts are added in their order.
-__device__ __noinline__ Sums add_parts(const float* all, int part_floats, int dh, int i, int first, int step, int count) {
+// Columns 4 i .. 4 i + 3 of an item (i counts over its heads) from `count` parts, `stride` floats apart, of which this thread adds first,
+// first + step, ... in their order.  The item's first part lies `ahead` floats further on than the others.  Eight parts' loads are in flight at a time.
+__device__ __noinline__ Sums add_parts(const float* all, size_t stride, int ahead, int dh, int i, int first, int step, int count) {
   Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
   const int ml_at = kHeads * dh + 2 * (4 * i / dh);
-  for (int c = first; c < count; c += 8 * step) {
-    float4 o[8];
-    float2 ml[8];
+  for (int c = first; c < count; c += kGroup * step) {
+    float4 o[kGroup];
+    float2 ml[kGroup];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
+    for (int q = 0; q < kGroup; ++q) {
       const int k = min(c + q * step, count - 1);
-      const float* x = all + (size_t)(2 * k + (k == 0)) * part_floats;      // the first block's part 1, part 0 behind it
+      const float* x = all + k * stride + (k == 0 ? ahead : 0);
       ml[q] = __ldcg(reinterpret_cast<const float2*>(x + ml_at));
       o[q] = __ldcg(reinterpret_cast<const float4*>(x) + i);
     }
     float m = a.m;
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
+    for (int q = 0; q < kGroup; ++q)
       if (c + q * step < count) m = fmaxf(m, ml[q].x);
     const Sums old = a;
     a = {make_float4(0.f, 0.f, 0.f, 0.f), m, 0.f};
     if (c != first) add_scaled(a, weight(old.m, m), old.o, old.l);
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
+    for (int q = 0; q < kGroup; ++q)
       if (c + q * step < count) add_scaled(a, weight(ml[q].x, m), o[q], ml[q].y);
   }
   return a;
 }
+
+// a * b / d, of which the product mostly has 32 bits (a 64-bit division is about 100 instructions)
+__device__ __forceinline__ long long mul_div(long long a, int b, long long d) {
+  const unsigned long long x = (unsigned long long)a * (unsigned)b;
+  return ((x | (unsigned long long)d) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : (long long)(x / (unsigned long long)d);
+}
+
+// The block that holds unit u when `total` units are spread over n blocks (block c begins at total * c / n).
+__device__ __forceinline__ int block_of(long long u, long long total, int n) {
+  const unsigned long long x = (unsigned long long)(u + 1) * (unsigned)n - 1;
+  return (int)(((x | (unsigned long long)total) >> 32) == 0 ? (uint32_t)x / (uint32_t)total : x / (unsigned long long)total);
+}
+
+// A sequence's units per item.
+__device__ __forceinline__ int span_of(int len) { return len == 0 ? 0 : (len + kUnit - 1) / kUnit + 1; }
 
 template <typename T, int DH, typename Item>
 __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_kernel(const __grid_constant__ AttendParams p) {
@@ -538,7 +552,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
   for (int s = s0; s < s1; ++s) {
     const int raw = p.lens[s];
     if ((raw < 0 || raw > p.cap) && p.status != nullptr) *p.status = AMPH_ERR_INVALID_ARG;
-    mine += (clamped_len(p, s) + kUnit - 1) / kUnit;
+    mine += span_of(clamped_len(p, s));
   }
   mine *= items;
   long long upto = mine;
@@ -564,12 +578,12 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
 
   const int n = (int)(total < gridDim.x ? total : gridDim.x);
   if ((int)blockIdx.x >= n) return;
-  const long long u0 = total * blockIdx.x / n, u1 = total * (blockIdx.x + 1) / n;
+  const long long u0 = mul_div(total, blockIdx.x, n), u1 = mul_div(total, blockIdx.x + 1, n);
   if (u0 >= before && u0 < before + mine) {
     long long at = before;
     int s = s0;
     for (;; ++s) {
-      const long long here = (long long)((clamped_len(p, s) + kUnit - 1) / kUnit) * items;
+      const long long here = (long long)span_of(clamped_len(p, s)) * items;
       if (u0 < at + here) break;
       at += here;
     }
@@ -579,17 +593,31 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
   __syncthreads();
   int seq = s_seq;
   long long u = u0;
-  int len = clamped_len(p, seq), tiles = (len + kUnit - 1) / kUnit;
-  int item = (int)((u0 - s_before) / tiles), tile = (int)((u0 - s_before) - (long long)item * tiles);
+  int len = clamped_len(p, seq), span = span_of(len);
+  int item = (int)mul_div(u0 - s_before, 1, span), at = (int)(u0 - s_before - (long long)item * span);
   while (u < u1) {
-    const int take = (int)(u1 - u < tiles - tile ? u1 - u : tiles - tile);
+    const int take = (int)(u1 - u < span - at ? u1 - u : span - at), tiles = span - 1;
+    const int t0 = max(at - 1, 0), t1 = at + take - 1;                  // keys [t0, t1) * kUnit
+    const long long first = u - at + 1;                                  // tile 0's place on the line
+    u += take;
+    at += take;
     const int kv = item / p.head_blocks, block0 = (item - kv * p.head_blocks) * kHeads;
     const int head0 = kv * p.group + block0, heads = min(kHeads, p.group - block0);
-    const int k0 = tile * kUnit, k1 = min(len, (tile + take) * kUnit);
-    Item::run(p, sm, mg, seq, kv, head0, heads, k0, k1);
-    const bool whole = take == tiles;
-    const long long first = u - tile;
-    float* part = p.parts + ((size_t)blockIdx.x * 2 + (tile == 0 ? 1 : 0)) * p.part_floats;
+    const int k0 = t0 * kUnit, k1 = min(len, t1 * kUnit), now = seq;
+    if (at == span) {
+      at = 0;
+      if (++item == items) {
+        item = 0;
+        if (u < u1) {
+          do ++seq; while ((len = clamped_len(p, seq)) == 0);
+          span = span_of(len);
+        }
+      }
+    }
+    if (t0 >= t1) continue;
+    Item::run(p, sm, mg, now, kv, head0, heads, k0, k1);
+    const bool whole = t1 - t0 == tiles;
+    float* part = p.parts + ((size_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * p.part_floats;
     const int slots = heads * DH / 4;
     for (int i = tid; i < slots; i += kAttThreads) {
       const int h = 4 * i / DH, c = 4 * i % DH;
@@ -600,61 +628,64 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
       for (int w = 0; w < kAttWarps; ++w)
         add_scaled(a, weight(mg.m[w][h], a.m), *reinterpret_cast<const float4*>(&mg.o[w][h][c]), mg.l[w][h]);
       if (whole) {
-        write_row<T, DH>(p, seq, head0 + h, c, a);
+        write_row<T, DH>(p, now, head0 + h, c, a);
       } else {
         reinterpret_cast<float4*>(part)[i] = a.o;
         if (c == 0) *reinterpret_cast<float2*>(part + kHeads * DH + 2 * h) = make_float2(a.m, a.l);
       }
     }
     if (!whole) {
-      const int c0 = block_of(first, total, n), c1 = block_of(first + tiles - 1, total, n);
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        s_last = atomicAdd(&p.counters[c0], 1) == c1 - c0;
-        if (s_last) p.counters[c0] = 0;
-      }
-      __syncthreads();
-      if (s_last) {
+      // The blocks of a group are neighbours; the last group has what is left, at least two blocks, so that no group begins where the next
+      // item may.
+      const int c0 = block_of(first, total, n), c1 = block_of(first + tiles - 1, total, n), count = c1 - c0 + 1;
+      const int groups = max(1, (count - 1) / kGroup), group = min(((int)blockIdx.x - c0) / kGroup, groups - 1);
+      const int g0 = c0 + group * kGroup, in_group = group == groups - 1 ? c1 - g0 + 1 : kGroup;
+      // adds up `parts` parts of p.counters[which]'s item or group if this block is the last one to get there
+      auto join = [&](int* counter, int parts, int from, int blocks_apart, bool done) {
         __threadfence();
-        const float* all = p.parts + (size_t)c0 * 2 * p.part_floats;
-        const int count = c1 - c0 + 1;
-        if (2 * slots <= kAttThreads) {           // few columns: several groups of threads share the parts
-          const int groups = kAttThreads / slots, group = tid / slots, i = tid - group * slots;
-          Sums a = {};
-          if (group < groups) {
-            a = add_parts(all, p.part_floats, DH, i, group, groups, count);
+        __syncthreads();
+        if (tid == 0) {
+          s_last = atomicAdd(counter, 1) == parts - 1;
+          if (s_last) *counter = 0;
+        }
+        __syncthreads();
+        if (!s_last) return false;
+        __threadfence();
+        float* all = p.parts + (size_t)from * 2 * p.part_floats;
+        const size_t stride = (size_t)blocks_apart * 2 * p.part_floats;
+        const int ahead = from == c0 ? p.part_floats : 0;
+        const int sharers = slots * 2 <= kAttThreads ? kAttThreads / slots : 1;      // few columns: several threads share the parts
+        for (int i0 = 0; i0 < slots; i0 += kAttThreads) {
+          const int sharer = sharers > 1 ? tid / slots : 0, i = sharers > 1 ? tid - sharer * slots : i0 + tid;
+          const bool mine_too = sharer < sharers && i < slots;
+          Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+          if (mine_too) a = add_parts(all, stride, ahead, DH, i, sharer, sharers, parts);
+          if (sharers > 1) {
             reinterpret_cast<float4*>(mg.o)[tid] = a.o;
             s_ml[tid] = make_float2(a.m, a.l);
           }
-          __syncthreads();
-          if (group == 0) {
-            float m = a.m;
-            for (int k = 1; k < groups; ++k) m = fmaxf(m, s_ml[k * slots + i].x);
-            Sums all_groups = {make_float4(0.f, 0.f, 0.f, 0.f), m, 0.f};
-            for (int k = 0; k < groups; ++k) {
-              const float2 ml = s_ml[k * slots + i];
-              add_scaled(all_groups, weight(ml.x, m), reinterpret_cast<const float4*>(mg.o)[k * slots + i], ml.y);
+          __syncthreads();                           // the parts have been read
+          if (mine_too && sharer == 0) {
+            if (sharers > 1) {
+              float m = a.m;
+              for (int k = 1; k < sharers; ++k) m = fmaxf(m, s_ml[k * slots + i].x);
+              a = {make_float4(0.f, 0.f, 0.f, 0.f), m, 0.f};
+              for (int k = 0; k < sharers; ++k) {
+                const float2 ml = s_ml[k * slots + i];
+                add_scaled(a, weight(ml.x, m), reinterpret_cast<const float4*>(mg.o)[k * slots + i], ml.y);
+              }
             }
-            write_row<T, DH>(p, seq, head0 + 4 * i / DH, 4 * i % DH, all_groups);
+            if (done) {
+              write_row<T, DH>(p, now, head0 + 4 * i / DH, 4 * i % DH, a);
+            } else {
+              reinterpret_cast<float4*>(all + ahead)[i] = a.o;
+              if (4 * i % DH == 0) *reinterpret_cast<float2*>(all + ahead + kHeads * DH + 2 * (4 * i / DH)) = make_float2(a.m, a.l);
+            }
           }
-        } else {
-          for (int i = tid; i < slots; i += kAttThreads)
-            write_row<T, DH>(p, seq, head0 + 4 * i / DH, 4 * i % DH, add_parts(all, p.part_floats, DH, i, 0, 1, count));
         }
-      }
-    }
-    u += take;
-    tile += take;
-    if (tile == tiles) {
-      tile = 0;
-      if (++item == items) {
-        item = 0;
-        if (u < u1) {
-          do ++seq; while ((len = clamped_len(p, seq)) == 0);
-          tiles = (len + kUnit - 1) / kUnit;
-        }
-      }
+        return true;
+      };
+      if (join(&p.counters[g0], in_group, g0, 1, groups == 1) && groups > 1) join(&p.counters[kMaxBlocks + c0], groups, c0, kGroup, true);
     }
     __syncthreads();
   }
@@ -726,7 +757,7 @@ cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
   return launch_pdl(paged_attention_kernel<T, DH, Item>, dim3(grid), dim3(kAttThreads), 0, st, p);
 }
 
-static_assert(kMaxBlocks * sizeof(int) <= AMPH_PAGED_WS_COUNTERS, "counters");
+static_assert(2 * kMaxBlocks * sizeof(int) <= AMPH_PAGED_WS_COUNTERS, "counters");
 static_assert(AMPH_PAGED_WS_COUNTERS + (size_t)kMaxBlocks * 2 * kHeads * (128 + 2) * sizeof(float) <= AMPH_PAGED_WS_BYTES, "parts");
 
 }  // namespace

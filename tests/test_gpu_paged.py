@@ -115,6 +115,15 @@ def test_attention(dtype, heads, kv, dh, page, lens):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv,dh,page,lens", [       # items cut into hundreds of parts, and into a few with whole ones around them
+    (8, 1, 128, 32, [40001]), (1, 1, 64, 64, [60000]), (5, 1, 128, 16, [1, 30000, 64]), (6, 2, 64, 256, [33333, 0, 2]), (11, 1, 128, 64, [25000]),
+    (2, 2, 128, 16, [1500, 64, 9000, 1, 65, 128, 7000, 3] * 3),
+])
+def test_attention_over_many_parts(dtype, heads, kv, dh, page, lens):
+    test_attention(dtype, heads, kv, dh, page, lens)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 def test_attention_of_many_sequences(dtype):
     """More sequences than threads in a block, most of them short, some empty; a table wider than any needs; a scale of one's own."""
     from paper_2406_13170_b200 import PagedCache, paged_attention
