@@ -218,11 +218,12 @@ __device__ __forceinline__ void halves(float v, bf16& hi, bf16& lo) {
 // `beside`: the kernel ahead is the tensor-core projection, which starts this one once everything ahead of itself is done, so it takes
 // the SMs and the shared memory that the projection leaves; only the first block waits for the projection, so that both are done when
 // this one is.  (Ahead of the projection, q / k / v of 64 rows of 24
-// tenants took 36.1 us in all, 28.1 now; gate / up of 37 rows at rank 64 48.5, 43.2 now.)
+// tenants took 36.1 us in all, 28.0 now; gate / up of 37 rows at rank 64 48.5, 44.2 now; 512 rows, see down_splits, 59 and 47.9.)  72 registers:
+// beside a CTA of the pair kernel an SM's schedulers have room for two such warps each, not for two of 80.
 // Bound: latency for a few rows, the adapters' bytes for many tenants.
 constexpr int kDownCols = 32;
 constexpr int kMaxDownSplits = 8;
-__global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const AdapterArgs p) {
+__global__ void __maxnreg__(72) adapter_down_kernel(const AdapterArgs p) {
   __shared__ union {
     TileSmem find;
     float red[kDownWarps][kTileRows][kDownCols + 2];
@@ -477,10 +478,11 @@ int most_tiles(int rows, int n_adapters) {
   const int64_t n = (int64_t)n_adapters + 1 + rows / kTileRows;
   return n < rows ? (int)n : rows;
 }
-// K ranges of adapter_down, a cluster: as many blocks as run at a time (three per SM), 64 columns of k for each warp at least
-int down_splits(int in, int blocks) {
+// K ranges of adapter_down, a cluster: at most `most` blocks in all, 64 columns of k for each warp at least.  444: three blocks per SM; 148
+// beside the pair kernel, which leaves room for one block per SM (512 rows, out 4096, in 11008, rank 32: 47.9 us with 148, 52.9 with 444).
+int down_splits(int in, int blocks, int most) {
   int s = 1;
-  while (s < kMaxDownSplits && s * kDownWarps * 64 < in && 2 * s * blocks <= 444) s *= 2;
+  while (s < kMaxDownSplits && s * kDownWarps * 64 < in && 2 * s * blocks <= most) s *= 2;
   return s;
 }
 size_t tiles_bytes(int rows) { return round256(sizeof(RowTile) * rows); }
@@ -560,7 +562,7 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   p.t_lo = p.t_hi + (size_t)rows * cols;
   p.y = y_dev;
   p.status = status_dev;
-  p.n_adapters = ad->n_adapters; p.rank = ad->rank; p.n_seg = n_seg; p.out = out; p.in = in; p.rows = rows; p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks);
+  p.n_adapters = ad->n_adapters; p.rank = ad->rank; p.n_seg = n_seg; p.out = out; p.in = in; p.rows = rows; p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks, use_tensor_core && rows > kWideFrom ? 148 : 444);
   PartialView pv;
   pv.p = (float*)((char*)ws_dev + tb);
   pv.ld = (int)ld;

@@ -669,6 +669,9 @@ int active_clusters(const TcGemm* g, const void* kernel, int ctas, size_t smem) 
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
   return n;
 }
+// A late trigger's successor has room beside a CTA of the plain form: for a block of 24 KB and, of 18 warps, for two warps of 72 registers
+// on each of an SM's four schedulers.
+constexpr size_t kLateRoom = 20 * 1024;
 template <int EPI>
 constexpr size_t ring_smem() { return EPI == WIDE_RESID ? kResidSmem : kWideSmem; }
 // Raises the shared memory limit of a form that is about to be launched, once per plan set: amph_project makes one per call, and three forms
@@ -760,7 +763,7 @@ bool wide_params(TcGemm* g, int xb, int n_seg, int tiles_per_seg, int in, int ro
   }
   prm->rows = rows;
   const size_t stage = kb * ((size_t)kTileM * 128 + (size_t)prm->n / 2 * 128);
-  prm->stages = (int)((ring_smem<EPI>() - 1024 - out_bytes) / stage);
+  prm->stages = (int)((ring_smem<EPI>() - (EPI == WIDE_PLAIN && g->late_trigger ? kLateRoom : 0) - 1024 - out_bytes) / stage);
   if (prm->stages > kMaxStages) prm->stages = kMaxStages;
   prm->flags = g->wide_flags;
   prm->wait_first = g->wait_first;
@@ -777,7 +780,7 @@ bool wide_run(TcGemm* g, const WideMaps& maps, const WideParams& prm, cudaStream
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * prm.groups * prm.nrb);
   cfg.blockDim = dim3(kWideThreads);
-  cfg.dynamicSmemBytes = ring_smem<EPI>();
+  cfg.dynamicSmemBytes = ring_smem<EPI>() - (EPI == WIDE_PLAIN && prm.late_trigger ? kLateRoom : 0);
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
