@@ -3,6 +3,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "amph_internal.cuh"
 
 namespace amph {
@@ -201,56 +203,108 @@ __device__ __forceinline__ void load_n(const float* p, float (&v)[2]) {
   const float2 a = *reinterpret_cast<const float2*>(p);
   v[0] = a.x; v[1] = a.y;
 }
+// 16 bytes to shared memory, zeros where `there` is false
+__device__ __forceinline__ void copy_async(float* dst, const float* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Keys [k0, k1) of one fp32 item by CUDA cores: scores with eight lanes per key, weighted values with every lane on its own columns.
+// The 16 keys at key0 as lanes see them: lane j (and j + 16) knows the page of key j, -1 where there is none.
+__device__ __forceinline__ int find_page(const AttendParams& p, int seq, int key0, int k1) {
+  const int key = key0 + (threadIdx.x & 15);
+  return key < k1 ? page_of(p, seq, key) : -1;
+}
+// Element offset of key j's row, from what find_page gave the lanes (all of them call)
+template <int DH>
+__device__ __forceinline__ int64_t row_of(const AttendParams& p, int kv, int key0, int page, int j) {
+  const int from = __shfl_sync(~0u, page, p.page_shift >= 4 ? 0 : j);           // pages of 16 slots or more: 16 keys share one
+  return ((((int64_t)from * p.n_kv + kv) << p.page_shift) + ((key0 + j) & ((1 << p.page_shift) - 1))) * DH;
+}
+
+// Keys [k0, k1) of one fp32 item by CUDA cores, 16 keys of a warp at a time through shared memory of its own: the next keys are copied while
+// these values are worked on, and the other way round.
+//   Scores   eight lanes share a key, four keys at a time of 16 held in registers, so that a query is read once for all of them
+//   Values   every lane has its own columns
+// Bound: HBM with few heads to a key, the issue of FMAs with eight (1300 instructions per 16 keys of 16 KB).  Eight ragged sequences of 40 heads
+// up to 2048 tokens: 78 us, 4.5 TB/s (185 us with every key loaded when it was needed).
 template <int DH>
 struct PlainItem {
   struct Smem {
+    union {
+      MergeSmem<DH> mg;
+      float kv[kAttWarps][2][16][DH];
+    };
     float q[kHeads][DH];
     float s[kAttWarps][kHeads][16];
     float alpha[kAttWarps][kHeads];
   };
-  static __device__ void run(const AttendParams& p, Smem& sm, MergeSmem<DH>& out, int seq, int kv, int head0, int heads, int k0, int k1) {
-    constexpr int C = DH / 32;
+  static __device__ __forceinline__ void run(const AttendParams& p, Smem& sm, int seq, int kv, int head0, int heads, int k0, int k1) {
+    constexpr int C = DH / 32, PER = 128 / DH;        // 128-byte parts of a key; keys that a warp copies at a time
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const float* kp = (const float*)p.k;
+    const float* vp = (const float*)p.v;
+    auto copy = [&](int which, int key0, int page, unsigned there) {
+      const float* src = which ? vp : kp;
+      const int mine = lane / (DH / 4), col = lane % (DH / 4) * 4;
+#pragma unroll
+      for (int j0 = 0; j0 < 16; j0 += PER) {
+        const int j = j0 + mine;
+        const int64_t at = row_of<DH>(p, kv, key0, page, j);
+        const bool is = (there >> j) & 1;
+        copy_async(&sm.kv[warp][which][j][col], is ? src + at + col : src, is);
+      }
+      commit_copies();
+    };
+    int key0 = k0 + warp * 16;
+    int page = find_page(p, seq, key0, k1);
+    unsigned there = __ballot_sync(~0u, page >= 0);
+    copy(0, key0, page, there);
+    copy(1, key0, page, there);
+    page = find_page(p, seq, key0 + kUnit, k1);
     for (int i = tid; i < heads * DH; i += kAttThreads)
       sm.q[i / DH][i % DH] = ((const float*)p.q)[((int64_t)seq * p.n_heads + head0) * DH + i];
     __syncthreads();
-    const float* kp = (const float*)p.k;
-    const float* vp = (const float*)p.v;
-    const int page_mask = (1 << p.page_shift) - 1;
     float o[kHeads][C];
 #pragma unroll
     for (int h = 0; h < kHeads; ++h)
 #pragma unroll
       for (int c = 0; c < C; ++c) o[h][c] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
-    const int my_head = lane >> 2;
-    for (int key0 = k0 + warp * 16; key0 < k1; key0 += kUnit) {
-      for (int i = 0; i < 4; ++i) {
-        const int j = i * 4 + (lane >> 3), key = key0 + j;
-        int page = -1;
-        if (key < k1) page = page_of(p, seq, key);
-        float kf[C][4];
+    const int my_head = lane >> 2, part = lane & 7;
+    for (; key0 < k1; key0 += kUnit) {
+      wait_copies<1>();
+      __syncwarp();
+      const unsigned now = there;
+      there = __ballot_sync(~0u, page >= 0);
+      float kf[4][C][4];                               // keys 4 i + lane / 8
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < C; ++c) load_n(&sm.kv[warp][0][4 * i + (lane >> 3)][c * 32 + part * 4], kf[i][c]);
+      __syncwarp();
+      copy(0, key0 + kUnit, page, there);
+      for (int h = 0; h < heads; ++h) {
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          if (page >= 0)
-            load_n(kp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + c * 32 + (lane & 7) * 4, kf[c]);
-          else
-            kf[c][0] = kf[c][1] = kf[c][2] = kf[c][3] = 0.f;
-        }
-        for (int h = 0; h < heads; ++h) {
-          float acc = 0.f;
+          const float4 qv = *reinterpret_cast<const float4*>(&sm.q[h][c * 32 + part * 4]);
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const float4 qv = *reinterpret_cast<const float4*>(&sm.q[h][c * 32 + (lane & 7) * 4]);
-            acc += kf[c][0] * qv.x; acc += kf[c][1] * qv.y; acc += kf[c][2] * qv.z; acc += kf[c][3] * qv.w;
+          for (int i = 0; i < 4; ++i) {
+            acc[i] += kf[i][c][0] * qv.x; acc[i] += kf[i][c][1] * qv.y; acc[i] += kf[i][c][2] * qv.z; acc[i] += kf[i][c][3] * qv.w;
           }
-          acc += __shfl_xor_sync(~0u, acc, 1);
-          acc += __shfl_xor_sync(~0u, acc, 2);
-          acc += __shfl_xor_sync(~0u, acc, 4);
-          if ((lane & 7) == 0) sm.s[warp][h][j] = page >= 0 ? acc * p.scale_log2 : -INFINITY;
         }
+        // sums over the eight lanes; bits 0 and 1 of the lane end up choosing which of the four keys it has
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float give = part & 1 ? acc[2 * i] : acc[2 * i + 1], keep = part & 1 ? acc[2 * i + 1] : acc[2 * i];
+          acc[i] = keep + __shfl_xor_sync(~0u, give, 1);
+        }
+        const float give = part & 2 ? acc[0] : acc[1], keep = part & 2 ? acc[1] : acc[0];
+        float x = keep + __shfl_xor_sync(~0u, give, 2);
+        x += __shfl_xor_sync(~0u, x, 4);
+        const int j = 4 * ((part & 2) + (part & 1)) + (lane >> 3);
+        if (part < 4) sm.s[warp][h][j] = (now >> j) & 1 ? x * p.scale_log2 : -INFINITY;
       }
       __syncwarp();
       if (my_head < heads) {
@@ -267,6 +321,7 @@ struct PlainItem {
         *reinterpret_cast<float4*>(&sm.s[warp][my_head][(lane & 3) * 4]) = s;
         if ((lane & 3) == 0) sm.alpha[warp][my_head] = alpha;
       }
+      wait_copies<1>();
       __syncwarp();
 #pragma unroll
       for (int h = 0; h < kHeads; ++h)
@@ -275,31 +330,37 @@ struct PlainItem {
 #pragma unroll
           for (int c = 0; c < C; ++c) o[h][c] *= alpha;
         }
-      for (int j = 0; j < 16 && key0 + j < k1; ++j) {
-        const int key = key0 + j, page = page_of(p, seq, key);
-        if (page < 0) continue;
-        float vf[C];
-        load_n(vp + ((((int64_t)page * p.n_kv + kv) << p.page_shift) + (key & page_mask)) * DH + lane * C, vf);
+#pragma unroll
+      for (int j0 = 0; j0 < 16; j0 += 4) {
+        float vf[4][C];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_n(&sm.kv[warp][1][j0 + j][lane * C], vf[j]);
 #pragma unroll
         for (int h = 0; h < kHeads; ++h)
           if (h < heads) {
-            const float w = sm.s[warp][h][j];
+            const float4 w = *reinterpret_cast<const float4*>(&sm.s[warp][h][j0]);
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[h][c] += w * vf[c];
+            for (int c = 0; c < C; ++c) {
+              o[h][c] += w.x * vf[0][c]; o[h][c] += w.y * vf[1][c]; o[h][c] += w.z * vf[2][c]; o[h][c] += w.w * vf[3][c];
+            }
           }
       }
       __syncwarp();
+      copy(1, key0 + kUnit, page, there);
+      page = find_page(p, seq, key0 + 2 * kUnit, k1);
     }
+    wait_copies<0>();
+    __syncthreads();                                   // the copies' place becomes the warps' results'
 #pragma unroll
     for (int h = 0; h < kHeads; ++h)
       if (h < heads)
 #pragma unroll
-        for (int c = 0; c < C; ++c) out.o[warp][h][lane * C + c] = o[h][c];
+        for (int c = 0; c < C; ++c) sm.mg.o[warp][h][lane * C + c] = o[h][c];
     l_run += __shfl_xor_sync(~0u, l_run, 1);
     l_run += __shfl_xor_sync(~0u, l_run, 2);
     if ((lane & 3) == 0) {
-      out.m[warp][my_head] = m_run;
-      out.l[warp][my_head] = l_run;
+      sm.mg.m[warp][my_head] = m_run;
+      sm.mg.l[warp][my_head] = l_run;
     }
     __syncthreads();
   }
@@ -332,14 +393,14 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
 // Bound: HBM.  A key's 4 head_dim bytes cost at most 16 head_dim * 4 flops, a tenth of what the tensor pipe does meanwhile.
 template <int DH>
 struct MmaItem {
-  struct Smem {};
-  static __device__ __forceinline__ void run(const AttendParams& p, Smem&, MergeSmem<DH>& out, int seq, int kv, int head0, int heads, int k0, int k1) {
+  struct Smem {
+    MergeSmem<DH> mg;
+  };
+  static __device__ __forceinline__ void run(const AttendParams& p, Smem& sm, int seq, int kv, int head0, int heads, int k0, int k1) {
     constexpr int C = DH / 64, W = DH / 16;          // 128-byte parts of a key; 32-bit words of a value row that a lane takes
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const bf16* kp = (const bf16*)p.k;
     const bf16* vp = (const bf16*)p.v;
-    const bool wide = p.page_shift >= 4;             // 16 keys share a page
-    const int page_mask = (1 << p.page_shift) - 1;
     uint32_t q[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -355,22 +416,12 @@ struct MmaItem {
     for (int j = 0; j < 2 * W; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
 
-    // lane j (and j + 16) knows the page of key j of the 16 at `key0`; -1: none
-    auto find = [&](int key0) {
-      const int key = key0 + (lane & 15);
-      return key < k1 ? page_of(p, seq, key) : -1;
-    };
-    // element offset of key j's row, and which keys of the 16 there are
-    auto row_of = [&](int key0, int page, int j) {
-      const int from = __shfl_sync(~0u, page, wide ? 0 : j);
-      return ((((int64_t)from * p.n_kv + kv) << p.page_shift) + ((key0 + j) & page_mask)) * DH;
-    };
     uint32_t kr[2][C][8], vr[4][W];
     auto load_k = [&](int key0, int page, unsigned there) {
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const int j = n * 8 + g;
-        const bf16* src = kp + row_of(key0, page, j) + t * 16;
+        const bf16* src = kp + row_of<DH>(p, kv, key0, page, j) + t * 16;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           if ((there >> j) & 1) {
@@ -386,7 +437,7 @@ struct MmaItem {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int j = 2 * t + (i & 1) + (i >> 1) * 8;
-        const bf16* src = vp + row_of(key0, page, j) + g * 2 * W;
+        const bf16* src = vp + row_of<DH>(p, kv, key0, page, j) + g * 2 * W;
         if ((there >> j) & 1) {
           load_once(src, vr[i]);
         } else {
@@ -396,11 +447,11 @@ struct MmaItem {
       }
     };
     int key0 = k0 + warp * 16;
-    int page = find(key0);
+    int page = find_page(p, seq, key0, k1);
     unsigned there = __ballot_sync(~0u, page >= 0);
     load_k(key0, page, there);
     load_v(key0, page, there);
-    int page_next = find(key0 + kUnit);
+    int page_next = find_page(p, seq, key0 + kUnit, k1);
     for (; key0 < k1; key0 += kUnit) {
       float s[2][4];
 #pragma unroll
@@ -449,7 +500,7 @@ struct MmaItem {
         mma_16816(o[j], hi[0], lo[0], hi[1], lo[1], __byte_perm(vr[0][j >> 1], vr[1][j >> 1], pick), __byte_perm(vr[2][j >> 1], vr[3][j >> 1], pick));
       }
       load_v(key0 + kUnit, page_next, there);
-      page_next = find(key0 + 2 * kUnit);
+      page_next = find_page(p, seq, key0 + 2 * kUnit, k1);
     }
     l_run += __shfl_xor_sync(~0u, l_run, 1);
     l_run += __shfl_xor_sync(~0u, l_run, 2);
@@ -458,11 +509,11 @@ struct MmaItem {
       for (int j = 0; j < 2 * W; j += 4)
 #pragma unroll
         for (int i = 0; i < 2; ++i)                   // columns 2 W n + j of n = 2 t + i
-          *reinterpret_cast<float4*>(&out.o[warp][g][2 * W * (2 * t + i) + j]) =
+          *reinterpret_cast<float4*>(&sm.mg.o[warp][g][2 * W * (2 * t + i) + j]) =
               make_float4(o[j][i] + o[j][i + 2], o[j + 1][i] + o[j + 1][i + 2], o[j + 2][i] + o[j + 2][i + 2], o[j + 3][i] + o[j + 3][i + 2]);
       if (t == 0) {
-        out.m[warp][g] = m_run;
-        out.l[warp][g] = l_run;
+        sm.mg.m[warp][g] = m_run;
+        sm.mg.l[warp][g] = l_run;
       }
     }
     __syncthreads();
@@ -537,8 +588,9 @@ template <typename T, int DH, typename Item>
 __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_kernel(const __grid_constant__ AttendParams p) {
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ MergeSmem<DH> mg;
-  __shared__ typename Item::Smem sm;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  typename Item::Smem& sm = *reinterpret_cast<typename Item::Smem*>(smem_raw);
+  MergeSmem<DH>& mg = sm.mg;
   __shared__ long long s_sum[kAttWarps], s_before;
   __shared__ int s_seq, s_last;
   __shared__ float2 s_ml[kAttThreads];
@@ -615,7 +667,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
       }
     }
     if (t0 >= t1) continue;
-    Item::run(p, sm, mg, now, kv, head0, heads, k0, k1);
+    Item::run(p, sm, now, kv, head0, heads, k0, k1);
     const bool whole = t1 - t0 == tiles;
     float* part = p.parts + ((size_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * p.part_floats;
     const int slots = heads * DH / 4;
@@ -754,7 +806,17 @@ cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   int grid = sms * kAttResident;
   if (grid > kMaxBlocks) grid = kMaxBlocks;
-  return launch_pdl(paged_attention_kernel<T, DH, Item>, dim3(grid), dim3(kAttThreads), 0, st, p);
+  constexpr size_t smem = sizeof(typename Item::Smem);
+  if (smem > 48 * 1024) {
+    static std::atomic<uint64_t> raised{0};            // devices whose limit has been raised
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev > 63 || !(raised.load() & bit)) {
+      e = cudaFuncSetAttribute(paged_attention_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e != cudaSuccess) return e;
+      raised.fetch_or(bit);
+    }
+  }
+  return launch_pdl(paged_attention_kernel<T, DH, Item>, dim3(grid), dim3(kAttThreads), smem, st, p);
 }
 
 static_assert(2 * kMaxBlocks * sizeof(int) <= AMPH_PAGED_WS_COUNTERS, "counters");
