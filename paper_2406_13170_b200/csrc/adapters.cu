@@ -3,6 +3,9 @@
 //   t[r][s][j] = sum_k x[r][k] a[i_r][s][j][k]                       the rows' low-rank products (down)
 //   P          = x . w^T                                             the projection kernels, as split-K partial sums
 //   y[r][s][o] = sum P + scale[i_r] sum_j t[r][s][j] b[i_r][s][o][j]  reduction of the partial sums, adapters' way back up (up)
+//
+// Small projections and those that the tensor-core kernels do not take: down, then all of y in one kernel (whole; fp32: the plain
+// projection's epilogue).
 #include <math.h>
 
 #include <mutex>
@@ -66,36 +69,6 @@ __global__ void __launch_bounds__(kThreads) adapter_down_plain_kernel(const Adap
 #pragma unroll
   for (int d = 16; d; d >>= 1) acc += __shfl_xor_sync(~0u, acc, d);
   if (lane == 0) p.t[(size_t)row * cols + col] = acc;
-}
-
-// fp32: grid (128 columns, row), one column per thread.
-__global__ void __launch_bounds__(kThreads) adapter_up_plain_kernel(const AdapterArgs p, const PartialView P) {
-  pdl_wait();
-  pdl_launch_dependents();
-  __shared__ float t[kMaxK * AMPH_MAX_ADAPTER_RANK];
-  const int cols = p.n_seg * p.rank, row = blockIdx.y, ld = p.n_seg * p.out;
-  const int i = adapter_of(p, row);
-  if (i >= 0) {
-    const float scale = p.scale ? p.scale[i] : 1.f;
-    for (int j = threadIdx.x; j < cols; j += kThreads) t[j] = scale * p.t[(size_t)row * cols + j];
-  }
-  __syncthreads();
-  const int c = blockIdx.x * kThreads + threadIdx.x;
-  if (c >= ld) return;
-  float acc = P.p[(size_t)row * P.ld + c];
-  if (i >= 0) {
-    const int seg = c / p.out, o = c - seg * p.out;
-    const float4* b = (const float4*)((const float*)p.b + (((size_t)i * p.n_seg + seg) * p.out + o) * p.rank);
-    const float* ts = t + seg * p.rank;
-    float low = 0.f;
-#pragma unroll 4
-    for (int j = 0; j < p.rank / 4; ++j) {
-      const float4 v = b[j];
-      low += ts[4 * j] * v.x; low += ts[4 * j + 1] * v.y; low += ts[4 * j + 2] * v.z; low += ts[4 * j + 3] * v.w;
-    }
-    acc += low;
-  }
-  ((float*)p.y)[(size_t)row * ld + c] = acc;
 }
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -461,6 +434,105 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
   }
 }
 
+// The whole of y behind adapter_down, for projections that are small or that the tensor-core kernels do not take: grid (32 columns, tile,
+// segment).  A block's warps share K, 64 of it at a time, and the rank, 32 of it at a time; both are terms of one sum of MMAs (rows as A,
+// weights or b as B, t in two halves), which meets in shared memory.  Every tile reads the weights again.  Bound: latency for small shapes,
+// else L2.
+struct Weights { const void* w[kMaxK]; };
+constexpr int kWholeCols = 32;
+template <bool VEC, typename TY>
+__global__ void __launch_bounds__(kThreads) adapter_whole_kernel(const __grid_constant__ AdapterArgs p, const __grid_constant__ Weights ws) {
+  pdl_wait();
+  pdl_launch_dependents();
+  constexpr int WARPS = kThreads / 32;
+  __shared__ __align__(16) float red[WARPS][kTileRows][kWholeCols + 4];
+  const RowTile& tile = p.tiles[blockIdx.y];
+  const int n = tile.n, adapter = tile.adapter, seg = blockIdx.z, c0 = blockIdx.x * kWholeCols;
+  if (n == 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int cols = p.n_seg * p.rank;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  auto load = [](const bf16* q) { return __ldg(reinterpret_cast<const uint4*>(q)); };
+  // Unconditional loads, as in adapter_up: a lane without a row or column reads the first row's or the last column's and writes nothing.
+  int row[2], o[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) row[i] = tile.row[g + 8 * i < n ? g + 8 * i : 0];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = min(c0 + (i >> 1) * 16 + 4 * (g >> 1) + 2 * (i & 1) + (g & 1), p.out - 1);
+  float acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+  const bf16 *x = (const bf16*)p.x, *w = (const bf16*)ws.w[seg];
+  const int steps = (p.in + 63) / 64;
+  for (int s = warp; s < steps; s += WARPS) {
+    uint4 xv[2][2], wv[4][2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int k = min(s * 64 + c * 32 + t * 8, p.in - 8);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) xv[i][c] = load(x + (size_t)row[i] * p.in + k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wv[i][c] = load(w + (size_t)o[i] * p.in + k);
+    }
+    if (s * 64 + 64 > p.in) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        if (s * 64 + c * 32 + t * 8 >= p.in) {
+          xv[0][c] = xv[1][c] = zero;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) wv[i][c] = zero;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        mma_16816(acc[i], xv[0][c].x, xv[1][c].x, xv[0][c].y, xv[1][c].y, wv[i][c].x, wv[i][c].y);
+        mma_16816(acc[i], xv[0][c].z, xv[1][c].z, xv[0][c].w, xv[1][c].w, wv[i][c].z, wv[i][c].w);
+      }
+  }
+  const int j = (warp * 4 + t) * 8;                     // rank is at most 32 for each of the four warps
+  static_assert(WARPS * 32 >= AMPH_MAX_ADAPTER_RANK, "every j has a warp");
+  if (adapter >= 0 && warp * 32 < p.rank) {
+    const bool is = j < p.rank;
+    const bf16* b = (const bf16*)p.b + ((size_t)adapter * p.n_seg + seg) * p.out * p.rank;
+    const int at = seg * p.rank + (is ? j : 0);
+    uint4 hi[2], lo[2], bv[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      hi[i] = *reinterpret_cast<const uint4*>(p.t_hi + (size_t)row[i] * cols + at);
+      lo[i] = *reinterpret_cast<const uint4*>(p.t_lo + (size_t)row[i] * cols + at);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bv[i] = load(b + (size_t)o[i] * p.rank + (is ? j : 0));
+    if (!is) {
+      hi[0] = hi[1] = lo[0] = lo[1] = zero;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bv[i] = zero;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      mma_16816(acc[i], lo[0].x, lo[1].x, lo[0].y, lo[1].y, bv[i].x, bv[i].y);
+      mma_16816(acc[i], lo[0].z, lo[1].z, lo[0].w, lo[1].w, bv[i].z, bv[i].w);
+      mma_16816(acc[i], hi[0].x, hi[1].x, hi[0].y, hi[1].y, bv[i].x, bv[i].y);
+      mma_16816(acc[i], hi[0].z, hi[1].z, hi[0].w, hi[1].w, bv[i].z, bv[i].w);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<float4*>(&red[warp][g + 8 * i][q * 16 + 4 * t]) =
+          make_float4(acc[2 * q][2 * i], acc[2 * q][2 * i + 1], acc[2 * q + 1][2 * i], acc[2 * q + 1][2 * i + 1]);
+  __syncthreads();
+  static_assert(kThreads * 4 == kTileRows * kWholeCols, "four sums a thread");
+  const int r = threadIdx.x / (kWholeCols / 4), c = threadIdx.x % (kWholeCols / 4) * 4, col = c0 + c;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int q = 0; q < WARPS; ++q) add4(sum, *reinterpret_cast<const float4*>(&red[q][r][c]));
+  if (r < n && col < p.out) put4<VEC>((TY*)p.y + (size_t)tile.row[r] * ((size_t)p.n_seg * p.out) + seg * p.out + col, sum, p.out - col);
+}
+
 constexpr int kMaxDevices = 64;
 std::mutex g_mutex;
 TcGemm* g_plans[kMaxDevices];            // tensor-map encoder and kernel attributes of a device; no call's data
@@ -473,6 +545,9 @@ int most_splits(int n_seg, int out) {
   const int s = (320 + tiles - 1) / tiles;
   return s > 16 ? 16 : s;
 }
+// Weights that adapter_whole's tiles may read in all.  Up to there its two launches take no longer than the tensor-core kernel's three and cost
+// the host 2.5 us less (three matrices of 512 x 512: 1 row 6.4 us, 6.8 with three; 128 rows, 19 MB, 8.3 and 8.5; 256 rows, 31 MB, 11.4 and 10.7).
+constexpr int64_t kWholeBytes = 24 << 20;
 // Tiles of rows that n_adapters adapters can make: each adapter, and the rows without one, rounds up once.
 int most_tiles(int rows, int n_adapters) {
   const int64_t n = (int64_t)n_adapters + 1 + rows / kTileRows;
@@ -514,6 +589,15 @@ cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaS
   return run_up<4, TY>(p, pv, tiles, st);
 }
 
+template <typename TY>
+cudaError_t run_whole(const AdapterArgs& p, const void* const* w, int tiles, cudaStream_t st) {
+  Weights ws = {};
+  for (int s = 0; s < p.n_seg; ++s) ws.w[s] = w[s];
+  const dim3 grid((p.out + kWholeCols - 1) / kWholeCols, tiles, p.n_seg);
+  return p.out % 4 == 0 ? launch_pdl(adapter_whole_kernel<true, TY>, grid, dim3(kThreads), 0, st, p, ws)
+                        : launch_pdl(adapter_whole_kernel<false, TY>, grid, dim3(kThreads), 0, st, p, ws);
+}
+
 cudaError_t run_down(const AdapterArgs& p, int tiles, int col_blocks, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(tiles, p.splits, col_blocks);
@@ -553,6 +637,8 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
     return api_fail(AMPH_ERR_WORKSPACE, "scratch: %zu bytes needed, 256-byte aligned", need);
   const size_t ld = (size_t)n_seg * out, tb = tiles_bytes(rows) + t_bytes(n_seg, rows, ad->rank);
   const int cols = n_seg * ad->rank, tiles = most_tiles(rows, ad->n_adapters), col_blocks = (cols + kDownCols - 1) / kDownCols;
+  // Small projections: adapter_whole instead of the tensor-core kernel and adapter_up (kWholeBytes).
+  const bool whole = dtype == AMPH_DTYPE_BF16 && (!use_tensor_core || (int64_t)tiles * n_seg * out * in * 2 <= kWholeBytes);
   AdapterArgs p;
   p.x = x_dev; p.a = ad->a; p.b = ad->b; p.scale = ad->scale;
   p.row_adapter = row_adapter;
@@ -562,7 +648,8 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   p.t_lo = p.t_hi + (size_t)rows * cols;
   p.y = y_dev;
   p.status = status_dev;
-  p.n_adapters = ad->n_adapters; p.rank = ad->rank; p.n_seg = n_seg; p.out = out; p.in = in; p.rows = rows; p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks, use_tensor_core && rows > kWideFrom ? 148 : 444);
+  p.n_adapters = ad->n_adapters; p.rank = ad->rank; p.n_seg = n_seg; p.out = out; p.in = in; p.rows = rows;
+  p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks, !whole && rows > kWideFrom ? 148 : 444);
   PartialView pv;
   pv.p = (float*)((char*)ws_dev + tb);
   pv.ld = (int)ld;
@@ -576,6 +663,8 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   if (use_tensor_core) {
     if (dtype != AMPH_DTYPE_BF16 || out % 128 || in % 64 || x_rows_cap < padded(rows))
       return api_fail(AMPH_ERR_SHAPE, "shape not covered by the tensor-core kernel");
+  }
+  if (use_tensor_core && !whole) {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) {
       cudaGetLastError();
@@ -612,14 +701,10 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   else
     e = run_down(p, tiles, col_blocks, st);
   if (e == cudaSuccess) {
-    if (!g) {
-      // the plain kernel takes blocks of up to kMaxRows rows as the context's passes do
-      GemmSeg segs[kMaxK];
-      for (int s = 0; s < n_seg; ++s) segs[s].w = w[s];
-      launch_gemm_generic(x_dev, in, segs, n_seg, out, in, P, (int)ld, rows, dtype, st);
-    }
     if (dtype == AMPH_DTYPE_F32)
-      e = launch_pdl(adapter_up_plain_kernel, dim3((unsigned)((ld + kThreads - 1) / kThreads), rows), dim3(kThreads), 0, st, p, pv);
+      e = launch_plain_adapters(x_dev, w, n_seg, out, in, (float*)y_dev, rows, {p.t, (const float*)p.b, p.scale, row_adapter, p.n_adapters, p.rank}, st);
+    else if (whole)
+      e = y_dtype == AMPH_DTYPE_F32 ? run_whole<float>(p, w, tiles, st) : run_whole<bf16>(p, w, tiles, st);
     else
       e = y_dtype == AMPH_DTYPE_F32 ? run_up<float>(p, pv, tiles, st) : run_up<bf16>(p, pv, tiles, st);
   }

@@ -224,6 +224,14 @@ struct GemmSeg { const void* w; };
 // kernel ahead in the stream has finished.
 void launch_gemm_generic(const void* x, int ldx, const GemmSeg* segs, int n_seg, int out, int in,
                          float* P, int ldp, int rows, int dtype, cudaStream_t st, int wait_first = 0);
+// The same in fp32 with each row's adapter in the epilogue: y[row][seg*out + o] = X[row] . W_seg[o] + scale[i] t[row][seg*rank + .] . b[i][seg][o][.],
+// i = row_adapter[row] (outside 0 .. n_adapters - 1: none).  Weights are read while the kernel ahead (which computes t) still runs.
+struct AdapterEpi {
+  const float *t, *b, *scale;
+  const int* row_adapter;
+  int n_adapters, rank;
+};
+cudaError_t launch_plain_adapters(const void* x, const void* const* w, int n_seg, int out, int in, float* y, int rows, const AdapterEpi& epi, cudaStream_t st);
 
 // fp32 projections whose kernel finishes the job: SwiGLU; rotary embedding and cache write; x += X . W^T with, if gain, xn <- gain * x
 // and ss[row][out / kPlainScaleCols] <- sums of squares (see RowScale).

@@ -697,7 +697,7 @@ constexpr int kPlainOneFeature = 296;    // blocks (two per SM) up to which a wa
 // its spread too.  RESID triggers at once: what follows it starts with weights that wait for nothing.
 // Us a step of an 8-layer model with separate kernels / with these forms: width 256, 16 rows 252 / 212, 512 rows 1338 / 1174; width
 // 512 402 / 369 and 2451 / 2406; width 1024 692 / 621 and 6167 / 6035; width 2048 1499 / 1331 and 19000 / 18337.
-enum { PLAIN_P = 0, PLAIN_SWIGLU = 1, PLAIN_ROPE = 2, PLAIN_RESID = 3 };
+enum { PLAIN_P = 0, PLAIN_SWIGLU = 1, PLAIN_ROPE = 2, PLAIN_RESID = 3, PLAIN_ADAPT = 4 };
 struct PlainEpi {
   RowScale rs;              // SWIGLU, ROPE: deferred division of the activation rows
   void* dst;                // SWIGLU: act [rows][out]; ROPE: q [rows][d]; RESID: xn [rows][out]
@@ -707,13 +707,14 @@ struct PlainEpi {
   float* x;                 // RESID [rows][out]
   const void* gain;         // RESID: or NULL (x only)
   float* ss;
+  AdapterEpi ad;            // ADAPT
 };
 
 template <typename T, int R, int O, int EPI>
 __global__ void __launch_bounds__(kPlainThreads)
 gemm_generic_kernel(const T* __restrict__ X, int ldx, const __grid_constant__ GemmSegs segs, int out, int in, float* __restrict__ P, int ldp, int rows,
                     int wait_first, const __grid_constant__ PlainEpi epi) {
-  if (EPI == PLAIN_P || EPI == PLAIN_RESID) pdl_launch_dependents();
+  if (EPI == PLAIN_P || EPI == PLAIN_RESID || EPI == PLAIN_ADAPT) pdl_launch_dependents();
   constexpr int V = Vec16<T>::N, KC = kPlainChunk / (int)sizeof(T);
   __shared__ __align__(16) uint4 xs[2][R][kPlainChunk / 16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -829,6 +830,24 @@ gemm_generic_kernel(const T* __restrict__ X, int ldx, const __grid_constant__ Ge
       const int rg = r0 + own_row();
       if (lane % same == 0 && rg < rows && o0 + i < out) P[(size_t)rg * ldp + blockIdx.y * out + o0 + i] = acc[i][0];
     }
+    if constexpr (EPI == PLAIN_ADAPT) {                  // the lanes of a row share the rank
+      const int rg = r0 + own_row(), rank = epi.ad.rank;
+      const bool is = rg < rows && o0 + i < out;
+      const int a = is ? epi.ad.row_adapter[rg] : -1;
+      float low = 0.f;
+      if (a >= 0 && a < epi.ad.n_adapters) {
+        const float* t = epi.ad.t + (size_t)rg * (gridDim.y * rank) + blockIdx.y * rank;
+        const float* b = epi.ad.b + (((size_t)a * gridDim.y + blockIdx.y) * out + o0 + i) * rank;
+        for (int j = lane % same * 4; j < rank; j += same * 4) {
+          const float4 u = *reinterpret_cast<const float4*>(t + j), v = *reinterpret_cast<const float4*>(b + j);
+          low += u.x * v.x; low += u.y * v.y; low += u.z * v.z; low += u.w * v.w;
+        }
+        if (epi.ad.scale != nullptr) low *= epi.ad.scale[a];
+      }
+#pragma unroll
+      for (int m = same / 2; m > 0; m >>= 1) low += __shfl_xor_sync(0xffffffffu, low, m);
+      if (lane % same == 0 && is) P[(size_t)rg * ldp + blockIdx.y * out + o0 + i] = acc[i][0] + low;
+    }
   }
   const int row = own_row(), rg = r0 + row;
   const bool mine = lane % same == 0 && rg < rows && o0 < out;
@@ -870,21 +889,32 @@ gemm_generic_kernel(const T* __restrict__ X, int ldx, const __grid_constant__ Ge
 // as those it has: 5 to 8 rows in blocks of 16 took 70 us at 11008 x 4096 in bf16, now 41; 102 at 3 x 4096 x 4096 in fp32, now 73); two
 // features a warp (half of the shared-memory reads) once one feature a warp gives more than two blocks per SM (8 rows: 51 us and
 // 82 us with one).
+template <typename T, int EPI>
+static cudaError_t run_plain(const T* X, int ldx, const GemmSegs& gs, int n_seg, int out, int in, float* P, int ldp, int rows, cudaStream_t st,
+                             int wait_first, const PlainEpi& epi) {
+  const int blocks = (out + 7) / 8;
+  auto run = [&](auto kernel, int R, int O) {
+    return launch_pdl(kernel, dim3((out + 8 * O - 1) / (8 * O), n_seg, (rows + R - 1) / R), dim3(kPlainThreads), 0, st, X, ldx, gs, out, in, P, ldp,
+                      rows, wait_first, epi);
+  };
+  if (rows <= 4) return run(gemm_generic_kernel<T, 4, 1, EPI>, 4, 1);
+  if (rows <= 8 && blocks * n_seg <= kPlainOneFeature) return run(gemm_generic_kernel<T, 8, 1, EPI>, 8, 1);
+  if (rows <= 8) return run(gemm_generic_kernel<T, 8, 2, EPI>, 8, 2);
+  if ((long long)blocks * n_seg * ((rows + 15) / 16) <= kPlainOneFeature) return run(gemm_generic_kernel<T, 16, 1, EPI>, 16, 1);
+  return run(gemm_generic_kernel<T, 16, 2, EPI>, 16, 2);
+}
 void launch_gemm_generic(const void* x, int ldx, const GemmSeg* segs, int n_seg, int out, int in, float* P,
                          int ldp, int rows, int dtype, cudaStream_t st, int wait_first) {
   GemmSegs gs;
   for (int s = 0; s < kMaxK; ++s) gs.s[s].w = s < n_seg ? segs[s].w : nullptr;
-  const int blocks = (out + 7) / 8;
-  auto run = [&](auto kernel, int R, int O, auto* X) {
-    launch_pdl(kernel, dim3((out + 8 * O - 1) / (8 * O), n_seg, (rows + R - 1) / R), dim3(kPlainThreads), 0, st, X, ldx, gs, out, in, P, ldp,
-               rows, wait_first, PlainEpi());
-  };
-  AMPH_DISPATCH(dtype, const T* X = (const T*)x;
-                if (rows <= 4) run(gemm_generic_kernel<T, 4, 1, PLAIN_P>, 4, 1, X);
-                else if (rows <= 8 && blocks * n_seg <= kPlainOneFeature) run(gemm_generic_kernel<T, 8, 1, PLAIN_P>, 8, 1, X);
-                else if (rows <= 8) run(gemm_generic_kernel<T, 8, 2, PLAIN_P>, 8, 2, X);
-                else if ((long long)blocks * n_seg * ((rows + 15) / 16) <= kPlainOneFeature) run(gemm_generic_kernel<T, 16, 1, PLAIN_P>, 16, 1, X);
-                else run(gemm_generic_kernel<T, 16, 2, PLAIN_P>, 16, 2, X));
+  AMPH_DISPATCH(dtype, run_plain<T, PLAIN_P>((const T*)x, ldx, gs, n_seg, out, in, P, ldp, rows, st, wait_first, PlainEpi()));
+}
+cudaError_t launch_plain_adapters(const void* x, const void* const* w, int n_seg, int out, int in, float* y, int rows, const AdapterEpi& ad, cudaStream_t st) {
+  GemmSegs gs;
+  for (int s = 0; s < kMaxK; ++s) gs.s[s].w = s < n_seg ? w[s] : nullptr;
+  PlainEpi epi = {};
+  epi.ad = ad;
+  return run_plain<float, PLAIN_ADAPT>((const float*)x, in, gs, n_seg, out, in, y, n_seg * out, rows, st, 0, epi);
 }
 
 // The fused forms, fp32: 16-row blocks, eight features (pairs) a block.  RESID only where launch_gemm_generic would take one feature a

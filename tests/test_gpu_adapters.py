@@ -108,6 +108,30 @@ def test_values(rows, n_seg, out, in_, rank, n, tc, dtype):
         assert bool(((y.double() - want).abs() <= TOL * big + 2.0 ** -8 * want.abs()).all())
 
 
+LARGE = [                                            # enough weights and rows for the tcgen05 kernels, odd tiles of both
+    (1, 8, 1024, 2048, 8, 1, True),
+    (5, 2, 2048, 2048, 16, 3, True),
+    (17, 1, 4096, 1408, 128, 2, True),
+    (64, 3, 2048, 1408, 64, 70, True),
+    (70, 3, 768, 1024, 8, 4, True),
+    (130, 1, 1024, 2048, 16, 2, True),
+    (512, 2, 1024, 512, 32, 3, True),
+    (333, 3, 2560, 576, 56, 40, True),
+    (300, 3, 1000, 520, 64, 20, False),
+]
+
+
+@pytest.mark.parametrize("which", ["mixed", "runs", "one", "none"])
+@pytest.mark.parametrize("rows,n_seg,out,in_,rank,n,tc", LARGE)
+def test_sums_of_whole_numbers_in_large(rows, n_seg, out, in_, rank, n, tc, which):
+    test_sums_of_whole_numbers(rows, n_seg, out, in_, rank, n, tc, which)
+
+
+@pytest.mark.parametrize("rows,n_seg,out,in_,rank,n,tc", LARGE)
+def test_values_in_large(rows, n_seg, out, in_, rank, n, tc):
+    test_values(rows, n_seg, out, in_, rank, n, tc, torch.bfloat16)
+
+
 @pytest.mark.parametrize("tc", [True, False], ids=["tcgen05", "plain"])
 def test_rows_do_not_meet_other_adapters(tc):
     """Adapters that no row names, and rows behind the last, may hold anything; so may the scratch."""
