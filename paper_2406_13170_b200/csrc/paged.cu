@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid
 // The work is a line of units of kUnit keys: sequence by sequence, in a sequence item by item (a key / value head and up to kHeads of
 // the query heads that share it), in an item unit by unit, with one unit more ahead of each item for what an item costs whatever its length
 // (the pipeline fills, the warps' sums are joined).  The grid is as many blocks as the device runs at a time, and
-// block c takes units [total * c / n, total * (c + 1) / n): every length mix is spread evenly, and the host needs no length.  An item
+// block c of n (the grid, or fewer where there is little) takes units [total * c / n, total * (c + 1) / n): every length mix is spread evenly, and the host needs no length.  An item
 // inside one block is finished there.  Of an item cut over blocks each leaves its part (running maximum, sum, weighted values)
 // in scratch.  Of every kGroup neighbouring parts the block that arrives last adds them in the order of the blocks, and of the groups the
 // one that is done last adds those: no block waits, and the bits do not depend on who is last.  Statistics and sums are fp32.
@@ -581,6 +581,70 @@ __device__ __forceinline__ int block_of(long long u, long long total, int n) {
   return (int)(((x | (unsigned long long)total) >> 32) == 0 ? (uint32_t)x / (uint32_t)total : x / (unsigned long long)total);
 }
 
+// Columns 4 i .. 4 i + 3 of an item from a block's warps
+template <int DH>
+__device__ __forceinline__ Sums join_warps(const MergeSmem<DH>& mg, int i) {
+  const int h = 4 * i / DH, c = 4 * i % DH;
+  Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), mg.m[0][h], 0.f};
+#pragma unroll
+  for (int w = 1; w < kAttWarps; ++w) a.m = fmaxf(a.m, mg.m[w][h]);
+#pragma unroll
+  for (int w = 0; w < kAttWarps; ++w)
+    add_scaled(a, weight(mg.m[w][h], a.m), *reinterpret_cast<const float4*>(&mg.o[w][h][c]), mg.l[w][h]);
+  return a;
+}
+
+// A few short sequences, where latency counts: grid (part, item, sequence), a cluster holds an item's parts and joins them through its
+// shared memory, every block an equal share of the columns.  No scratch, no line to find one's place on.  (One sequence of 640 tokens, 32 heads:
+// 6.1 us, 9.0 with the line; see kShortKeys.)
+constexpr int kMaxParts = 16;
+template <typename T, int DH, typename Item>
+__global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_cluster_kernel(const __grid_constant__ AttendParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  typename Item::Smem& sm = *reinterpret_cast<typename Item::Smem*>(smem_raw);
+  constexpr int kMost = kHeads * DH / 4;
+  __shared__ __align__(16) float4 o_in[kMost + kMaxParts];             // [part][share]
+  __shared__ float2 ml_in[kMost + kMaxParts];
+  const int tid = threadIdx.x, parts = gridDim.x, part = blockIdx.x, seq = blockIdx.z;
+  const int kv = blockIdx.y / p.head_blocks, block0 = (blockIdx.y - kv * p.head_blocks) * kHeads;
+  const int head0 = kv * p.group + block0, heads = min(kHeads, p.group - block0), slots = heads * DH / 4;
+  const int raw = p.lens[seq], len = raw < 0 ? 0 : min(raw, p.cap);
+  if (raw != len && p.status != nullptr && tid == 0) *p.status = AMPH_ERR_INVALID_ARG;
+  if (len == 0) {                                                      // the same in the whole cluster
+    if (part == 0)
+      for (int i = tid; i < slots; i += kAttThreads) write_row<T, DH>(p, seq, head0 + 4 * i / DH, 4 * i % DH, Sums{});
+    return;
+  }
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  const int units = (len + kUnit - 1) / kUnit, k0 = units * part / parts * kUnit, k1 = min(len, units * (part + 1) / parts * kUnit);
+  if (k0 < k1) Item::run(p, sm, seq, kv, head0, heads, k0, k1);
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");          // every block has begun
+  const int share = (slots + parts - 1) / parts;
+  for (int i = tid; i < slots; i += kAttThreads) {
+    Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+    if (k0 < k1) a = join_warps<DH>(sm.mg, i);
+    const int to = i / share, at = part * share + i - to * share;
+    uint32_t o_at, ml_at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(o_at) : "r"((uint32_t)__cvta_generic_to_shared(&o_in[at])), "r"(to));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ml_at) : "r"((uint32_t)__cvta_generic_to_shared(&ml_in[at])), "r"(to));
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(o_at), "f"(a.o.x), "f"(a.o.y), "f"(a.o.z), "f"(a.o.w) : "memory");
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(ml_at), "f"(a.m), "f"(a.l) : "memory");
+  }
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  for (int j = tid; j < share; j += kAttThreads) {
+    const int i = part * share + j;
+    if (i >= slots) break;
+    float m = -INFINITY;
+    for (int k = 0; k < parts; ++k) m = fmaxf(m, ml_in[k * share + j].x);
+    Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), m, 0.f};
+    for (int k = 0; k < parts; ++k) add_scaled(a, weight(ml_in[k * share + j].x, m), o_in[k * share + j], ml_in[k * share + j].y);
+    write_row<T, DH>(p, seq, head0 + 4 * i / DH, 4 * i % DH, a);
+  }
+}
+
 // A sequence's units per item.
 __device__ __forceinline__ int span_of(int len) { return len == 0 ? 0 : (len + kUnit - 1) / kUnit + 1; }
 
@@ -628,7 +692,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
     if (clamped_len(p, s) == 0)
       for (int i = tid; i < p.n_heads * DH / 4; i += kAttThreads) write_row<T, DH>(p, s, 4 * i / DH, 4 * i % DH, Sums{});
 
-  const int n = (int)(total < gridDim.x ? total : gridDim.x);
+  const int n = (int)(total < 2 * gridDim.x ? (total + 1) / 2 : gridDim.x);       // two units a block at least: fewer parts
   if ((int)blockIdx.x >= n) return;
   const long long u0 = mul_div(total, blockIdx.x, n), u1 = mul_div(total, blockIdx.x + 1, n);
   if (u0 >= before && u0 < before + mine) {
@@ -673,12 +737,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_ker
     const int slots = heads * DH / 4;
     for (int i = tid; i < slots; i += kAttThreads) {
       const int h = 4 * i / DH, c = 4 * i % DH;
-      Sums a = {make_float4(0.f, 0.f, 0.f, 0.f), mg.m[0][h], 0.f};
-#pragma unroll
-      for (int w = 1; w < kAttWarps; ++w) a.m = fmaxf(a.m, mg.m[w][h]);
-#pragma unroll
-      for (int w = 0; w < kAttWarps; ++w)
-        add_scaled(a, weight(mg.m[w][h], a.m), *reinterpret_cast<const float4*>(&mg.o[w][h][c]), mg.l[w][h]);
+      const Sums a = join_warps<DH>(mg, i);
       if (whole) {
         write_row<T, DH>(p, now, head0 + h, c, a);
       } else {
@@ -798,6 +857,11 @@ cudaError_t run_write(const WriteParams& p, int rows, cudaStream_t st) {
   return (int64_t)rows * items <= 148 * 4 * kWriteThreads ? run_write_items<TS, TD, 1>(p, rows, items, st) : run_write_items<TS, TD, 3>(p, rows, items, st);
 }
 
+// What the table has room for, up to which an item gets a cluster: keys of a block, bytes of all keys and values.  Captured, line / cluster: one
+// sequence of 640 tokens, 32 heads 9.0 / 6.1 us, 16 of 800 with 8 heads to one of 64 8.2 / 5.0, one of 2000 with 8 heads to one 14.0 / 6.0, of
+// 8000 16.7 / 13.0, of 30000 26 / 37; 33 MB (8 of 2000, 32 / 8 heads) 15.5 / 18.7.
+constexpr int kShortKeys = 8 * kUnit;
+constexpr int64_t kShortBytes = 16 << 20;
 template <typename T, int DH, typename Item>
 cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
   int dev = 0, sms = 0;
@@ -807,14 +871,38 @@ cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
   int grid = sms * kAttResident;
   if (grid > kMaxBlocks) grid = kMaxBlocks;
   constexpr size_t smem = sizeof(typename Item::Smem);
-  if (smem > 48 * 1024) {
-    static std::atomic<uint64_t> raised{0};            // devices whose limit has been raised
+  {
+    static std::atomic<uint64_t> ready{0};             // devices on which the kernels have their attributes
     const uint64_t bit = 1ull << (dev & 63);
-    if (dev > 63 || !(raised.load() & bit)) {
-      e = cudaFuncSetAttribute(paged_attention_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (dev > 63 || !(ready.load() & bit)) {
+      e = cudaFuncSetAttribute(paged_attention_cluster_kernel<T, DH, Item>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_cluster_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       if (e != cudaSuccess) return e;
-      raised.fetch_or(bit);
+      ready.fetch_or(bit);
     }
+  }
+  // A cluster for each item where all of them run at once and the tables have room for few keys
+  const int64_t items = (int64_t)p.n_seqs * p.n_kv * p.head_blocks;
+  int parts = items <= grid ? (int)(grid / items) : 0;
+  if (parts > (p.cap + kUnit - 1) / kUnit) parts = (p.cap + kUnit - 1) / kUnit;
+  if (parts > kMaxParts) parts = kMaxParts;
+  if (p.cap <= parts * kShortKeys && (int64_t)p.n_seqs * p.n_kv * p.cap * DH * (2 * sizeof(T)) <= kShortBytes) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(parts, p.n_kv * p.head_blocks, p.n_seqs);
+    cfg.blockDim = dim3(kAttThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = parts;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, paged_attention_cluster_kernel<T, DH, Item>, p);
   }
   return launch_pdl(paged_attention_kernel<T, DH, Item>, dim3(grid), dim3(kAttThreads), smem, st, p);
 }

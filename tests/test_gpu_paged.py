@@ -115,6 +115,32 @@ def test_attention(dtype, heads, kv, dh, page, lens):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv,dh,page,lens", ATTEND)
+def test_short_sequences_in_wide_tables(dtype, heads, kv, dh, page, lens):
+    """The table's width chooses the kernel: these have room for 150,000 tokens."""
+    from paper_2406_13170_b200 import PagedCache, paged_attention
+    g = _gen(heads * 17 + len(lens))
+    table, n_pages = _table(lens, page, g, width=-(-150000 // page))
+    kp, vp = _normal(g, n_pages, kv, page, dh, dtype=dtype), _normal(g, n_pages, kv, page, dh, dtype=dtype)
+    q = _normal(g, len(lens), heads, dh, dtype=dtype, std=2.0)
+    lse = torch.full((len(lens), heads), 7.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = paged_attention(PagedCache(kp, vp), q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), lse=lse, status=status)
+    assert int(status) == 0
+    _check_attention(out, lse, q, kp, vp, table, lens)
+    # absent pages and lengths that do not exist, in this kernel too
+    bad = table.clone()
+    bad[:, 0] = n_pages
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out2 = paged_attention(PagedCache(kp, vp), q, bad, n, status=status)
+    assert int(status) == (1 if max(lens) > 0 else 0) and torch.isfinite(out2.float()).all()
+    n[-1] = -5
+    status.zero_()
+    out2 = paged_attention(PagedCache(kp, vp), q, table, n, status=status)
+    assert int(status) == 1 and not out2[-1].any() and torch.equal(out2[:-1], paged_attention(PagedCache(kp, vp), q, table, n)[:-1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("heads,kv,dh,page,lens", [       # items cut into hundreds of parts, and into a few with whole ones around them
     (8, 1, 128, 32, [40001]), (1, 1, 64, 64, [60000]), (5, 1, 128, 16, [1, 30000, 64]), (6, 2, 64, 256, [33333, 0, 2]), (11, 1, 128, 64, [25000]),
     (2, 2, 128, 16, [1500, 64, 9000, 1, 65, 128, 7000, 3] * 3),
