@@ -553,8 +553,9 @@ int most_tiles(int rows, int n_adapters) {
   const int64_t n = (int64_t)n_adapters + 1 + rows / kTileRows;
   return n < rows ? (int)n : rows;
 }
-// K ranges of adapter_down, a cluster: at most `most` blocks in all, 64 columns of k for each warp at least.  444: three blocks per SM; 148
-// beside the pair kernel, which leaves room for one block per SM (512 rows, out 4096, in 11008, rank 32: 47.9 us with 148, 52.9 with 444).
+// K ranges of adapter_down, a cluster: at most `most` blocks in all, 64 columns of k for each warp at least.  444: three blocks per SM; 168
+// beside the pair kernel, which leaves room for one block on each SM that it uses (512 rows, out 4096, in 11008, rank 32: 47.9 us, 52.9 with 444;
+// 128 rows, three matrices of 5120 x 5120, rank 16, 32 adapters: 43.7 us, 54.3 with 148 and so no cluster).
 int down_splits(int in, int blocks, int most) {
   int s = 1;
   while (s < kMaxDownSplits && s * kDownWarps * 64 < in && 2 * s * blocks <= most) s *= 2;
@@ -649,7 +650,7 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
   p.y = y_dev;
   p.status = status_dev;
   p.n_adapters = ad->n_adapters; p.rank = ad->rank; p.n_seg = n_seg; p.out = out; p.in = in; p.rows = rows;
-  p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks, !whole && rows > kWideFrom ? 148 : 444);
+  p.splits = dtype == AMPH_DTYPE_F32 ? 1 : down_splits(in, tiles * col_blocks, !whole && rows > kWideFrom ? 168 : 444);
   PartialView pv;
   pv.p = (float*)((char*)ws_dev + tb);
   pv.ld = (int)ld;

@@ -153,7 +153,9 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid
 constexpr int kUnit = 64;                // keys: 16 for each warp
 constexpr int kAttWarps = 4;
 constexpr int kAttThreads = kAttWarps * 32;
-constexpr int kAttResident = 3;          // blocks per SM: 168 registers a thread
+// blocks per SM: 168 or 128 registers a thread; those of 64 columns have half the bytes in flight (16 sequences up to 4000, 32 heads: 54.5 us, 60.3
+// with three)
+template <int DH> constexpr int kAttResident = DH == 64 ? 4 : 3;
 constexpr int kHeads = 8;                // query heads of an item
 constexpr int kMaxBlocks = 592;
 constexpr int kGroup = 8;                // parts that one block adds at a time: as many as it has loads in flight
@@ -599,7 +601,7 @@ __device__ __forceinline__ Sums join_warps(const MergeSmem<DH>& mg, int i) {
 // 6.1 us, 9.0 with the line; see kShortKeys.)
 constexpr int kMaxParts = 16;
 template <typename T, int DH, typename Item>
-__global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_cluster_kernel(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(kAttThreads, kAttResident<DH>) paged_attention_cluster_kernel(const __grid_constant__ AttendParams p) {
   pdl_wait();
   pdl_launch_dependents();
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -649,7 +651,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_clu
 __device__ __forceinline__ int span_of(int len) { return len == 0 ? 0 : (len + kUnit - 1) / kUnit + 1; }
 
 template <typename T, int DH, typename Item>
-__global__ void __launch_bounds__(kAttThreads, kAttResident) paged_attention_kernel(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(kAttThreads, kAttResident<DH>) paged_attention_kernel(const __grid_constant__ AttendParams p) {
   pdl_wait();
   pdl_launch_dependents();
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -864,24 +866,21 @@ constexpr int kShortKeys = 8 * kUnit;
 constexpr int64_t kShortBytes = 16 << 20;
 template <typename T, int DH, typename Item>
 cudaError_t run_attention(const AttendParams& p, cudaStream_t st) {
-  int dev = 0, sms = 0;
+  int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
-  int grid = sms * kAttResident;
-  if (grid > kMaxBlocks) grid = kMaxBlocks;
   constexpr size_t smem = sizeof(typename Item::Smem);
-  {
-    static std::atomic<uint64_t> ready{0};             // devices on which the kernels have their attributes
-    const uint64_t bit = 1ull << (dev & 63);
-    if (dev > 63 || !(ready.load() & bit)) {
-      e = cudaFuncSetAttribute(paged_attention_cluster_kernel<T, DH, Item>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_cluster_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != cudaSuccess) return e;
-      ready.fetch_or(bit);
-    }
+  static std::atomic<int> known[64];                   // multiprocessors of a device on which the kernels have their attributes
+  int sms = dev < 64 ? known[dev].load() : 0;
+  if (sms == 0) {
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_cluster_kernel<T, DH, Item>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_cluster_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attention_kernel<T, DH, Item>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) known[dev].store(sms);
   }
+  const int grid = sms * kAttResident<DH> < kMaxBlocks ? sms * kAttResident<DH> : kMaxBlocks;
   // A cluster for each item where all of them run at once and the tables have room for few keys
   const int64_t items = (int64_t)p.n_seqs * p.n_kv * p.head_blocks;
   int parts = items <= grid ? (int)(grid / items) : 0;
