@@ -226,6 +226,7 @@ PyObject* paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (qs < 0 || heads > 0x7fffffff || (q_in && !whole(q_in, dev, scalar(c->c.dtype), {rows, heads, dh}))) return not_these();
     q_out = q_in ? *q_in : make({rows, heads, dh}, scalar(c->c.dtype), dev);
   }
+  if (rows == 0) return give(q_out, AMPH_OK);            // (an empty tensor has no address)
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
   return give(q_out, lib.paged_write(&c->c, q ? q->data_ptr() : nullptr, qs, k->data_ptr(), ks, v->data_ptr(), vs, amph_dtype(type), (int)heads, (int)rows,
                                      (const int32_t*)seq->data_ptr(), (const int32_t*)pos->data_ptr(), (const int32_t*)table->data_ptr(),
@@ -255,12 +256,13 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return not_these();
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)dev);
   const at::Tensor out = out_in ? *out_in : make(q->sizes(), type, dev);
+  if (seqs == 0) return give(out, AMPH_OK);              // (an empty tensor has no address)
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
   Scratch& ws = scratch(FOR_ATTENTION, dev, stream, AMPH_PAGED_WS_BYTES);
   const int rc = lib.paged_attention(&c->c, q->data_ptr(), (int)heads, (const int32_t*)lens->data_ptr(), (const int32_t*)table->data_ptr(), (int)seqs,
                                      (int)table->size(1), (float)scale, out.data_ptr(), lse ? (float*)lse->data_ptr() : nullptr, ws.t.data_ptr(),
                                      AMPH_PAGED_WS_BYTES, ws.clean, status ? (int32_t*)status->data_ptr() : nullptr, stream);
-  ws.clean = rc == AMPH_OK && (ws.clean || seqs > 0);
+  ws.clean = rc == AMPH_OK;
   return give(out, rc);
   END_HANDLE_TH_ERRORS
 }

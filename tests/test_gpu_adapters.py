@@ -197,6 +197,52 @@ def test_side_stream_and_capture():
     assert torch.equal(out, project_adapters(x, w, 50, True, ad, at)) and not torch.equal(out, want)
 
 
+def test_two_graphs_beside_one_another():
+    """Replayed at the same time on two streams, each with its own scratch; the same calls outside at the same time."""
+    from paper_2406_13170_b200 import Adapters, project_adapters
+    g = torch.Generator(device=DEV).manual_seed(8)
+    sets = []
+    for rows, n_seg, out, in_, rank in ((50, 3, 2048, 1024, 16), (200, 2, 1024, 2048, 32)):
+        x, w = _ints(g, -1, 1, _cap(rows), in_, dtype=torch.bfloat16), [_ints(g, -2, 2, out, in_, dtype=torch.bfloat16) for _ in range(n_seg)]
+        ad = Adapters(_ints(g, -1, 1, 5, n_seg, rank, in_, dtype=torch.bfloat16), _ints(g, -1, 1, 5, n_seg, out, rank, dtype=torch.bfloat16))
+        at = torch.tensor([r * 7 % 6 - 1 for r in range(rows)], dtype=torch.int32, device=DEV)
+        sets.append((x, w, rows, True, ad, at))
+    want = [project_adapters(*s) for s in sets]
+    graphs, outs = [], []
+    for s in sets:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            outs.append([project_adapters(*s) for _ in range(2)])
+        graphs.append(gr)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    eager = []
+    for _ in range(6):
+        for gr, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                gr.replay()
+        eager.append([project_adapters(*s) for s in sets])
+    torch.cuda.synchronize()
+    for i, w in enumerate(want):
+        assert all(torch.equal(o, w) for o in outs[i]) and all(torch.equal(e[i], w) for e in eager)
+
+
+def test_an_output_as_the_next_call_s_weights():
+    """What a call leaves is there for the next one, whatever it takes it for."""
+    from paper_2406_13170_b200 import Adapters, project_adapters
+    g = torch.Generator(device=DEV).manual_seed(9)
+    rows, d = 512, 512
+    x, w = _ints(g, -1, 1, rows, d, dtype=torch.bfloat16), _ints(g, -1, 1, d, d, dtype=torch.bfloat16)
+    ad = Adapters(_ints(g, 0, 1, 1, 1, 8, d, dtype=torch.bfloat16) * 0, _ints(g, -1, 1, 1, 1, d, 8, dtype=torch.bfloat16))
+    at = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    for _ in range(20):
+        y = project_adapters(x, [w], rows, True, ad, at)                       # [512, 512]: whole numbers below 2^8 are exact in bf16
+        z = project_adapters(x, [y], rows, True, ad, at, y_dtype=torch.float32)
+        want = x.double() @ (x.double() @ w.double().T).to(torch.bfloat16).double().T
+        assert torch.equal(z.double(), want)
+        x = x.roll(1, 0)
+
+
 def test_python_refusals():
     from paper_2406_13170_b200 import Adapters, AmphError, project_adapters
     z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device=DEV)        # noqa: E731

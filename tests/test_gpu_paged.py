@@ -449,6 +449,74 @@ def test_captured_and_replayed_beside_one_another():
             assert torch.equal(o, w)
 
 
+LONG = [(9000, 37, 0, 30001), (20000, 1, 12345, 700)]        # many parts: through scratch
+
+
+def test_two_streams_over_many_parts():
+    from paper_2406_13170_b200 import paged_attention
+    sets = [_setup(61, lens=LONG[0]), _setup(62, lens=LONG[1])]
+    want = [paged_attention(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(30):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(paged_attention(*sets[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in got[i])
+
+
+def test_graphs_of_several_calls_beside_one_another_and_eager_ones():
+    """Calls of one capture share scratch; graphs, and the calls outside them, do not."""
+    from paper_2406_13170_b200 import paged_attention
+    sets = [_setup(63, lens=LONG[0]), _setup(64, lens=LONG[1])]
+    graphs, outs = [], []
+    for s in sets:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            outs.append([paged_attention(*s) for _ in range(3)])
+        graphs.append(gr)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for step in range(3):
+        for c, q, table, lens in sets:
+            q.mul_(0.9)
+            lens.copy_((lens - 77 * step).clamp(min=0))
+        want = [paged_attention(*s) for s in sets]
+        torch.cuda.synchronize()
+        eager = []
+        for _ in range(4):
+            for gr, st in zip(graphs, streams):
+                with torch.cuda.stream(st):
+                    gr.replay()
+            eager.append([paged_attention(*s) for s in sets])
+        torch.cuda.synchronize()
+        for i, w in enumerate(want):
+            assert all(torch.equal(o, w) for o in outs[i]) and all(torch.equal(e[i], w) for e in eager)
+
+
+def test_empty_batches():
+    from paper_2406_13170_b200 import paged_attention, paged_write
+    c, q, table, lens = _setup(65)
+    before = c.k_pages.clone()
+    assert paged_attention(c, q[:0], table[:0], lens[:0]).shape == (0, 8, 128)
+    k = torch.zeros(0, 256, device=DEV, dtype=torch.bfloat16)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    assert paged_write(c, None, k, k, none, none, table) is None
+    assert paged_write(c, k.repeat(1, 4), k, k, none, none, table).shape == (0, 8, 128)
+    assert torch.equal(c.k_pages, before)
+
+
+def test_pages_have_to_be_aligned():
+    from paper_2406_13170_b200 import AmphError, PagedCache, paged_attention
+    c, q, table, lens = _setup(66)
+    flat = torch.zeros(c.k_pages.numel() + 8, dtype=torch.bfloat16, device=DEV)
+    odd = flat[8:].view(c.k_pages.shape)
+    with pytest.raises(AmphError, match="32-byte"):
+        paged_attention(PagedCache(odd, c.v_pages), q, table, lens)
+
+
 def test_python_refusals():
     from paper_2406_13170_b200 import AmphError, PagedCache, paged_attention, paged_write
     c, q, table, lens = _setup(51)
