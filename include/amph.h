@@ -349,7 +349,8 @@ typedef struct {
 
 /* y[r][s*out + o] = sum_k x[r][k] w[s][o][k] + scale[i] sum_j (sum_k x[r][k] a[i][s][j][k]) b[i][s][o][j],  i = row_adapter[r]
  * (device int32 [rows], any order; negative: the row has no adapter; >= n_adapters: the same, and status_dev is set).
- * x, w, n_seg, out, in, rows (1..512), x_rows_cap, dtype and use_tensor_core as for amph_project.  y: [rows][n_seg*out] of
+ * x, w, n_seg, out, in, rows (1..512), x_rows_cap, dtype and use_tensor_core as for amph_project (small bf16 projections, and those with
+ * use_tensor_core = 0, run on the warp-level tensor cores).  y: [rows][n_seg*out] of
  * y_dtype, 16-byte aligned (AMPH_DTYPE_F32, or AMPH_DTYPE_BF16 with bf16 weights: the sums, held in fp32, are rounded once).
  * ws_dev: device scratch, 256-byte aligned, at least amph_project_adapters_bytes() bytes; nothing in it needs to be set and nothing
  * is kept in it.  Calls that may overlap on the GPU need scratch of their own.  Make the first call on a device outside a stream capture. */
@@ -389,7 +390,8 @@ amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64
  * n_seqs at most AMPH_PAGED_MAX_SEQS.  ws_dev: device scratch of AMPH_PAGED_WS_BYTES, 256-byte aligned, for the parts of sequences that several
  * blocks share.  Its first AMPH_PAGED_WS_COUNTERS bytes must be zero when the kernel starts, and every call leaves them zero: with
  * ws_clean = 0 the call clears them itself (scratch with any contents), with ws_clean = 1 the caller vouches for them (cleared
- * once, used by these calls alone).  Calls that may overlap on the GPU need scratch of their own.  Equal inputs give equal bits. */
+ * once, used by these calls alone).  Calls that may overlap on the GPU need scratch of their own.  Equal inputs give equal bits.
+ * Slots behind a sequence's length are never read.  A value of V that is infinite makes its column infinite or NaN. */
 #define AMPH_PAGED_MAX_SEQS 4096
 #define AMPH_PAGED_WS_COUNTERS 8192u
 #define AMPH_PAGED_WS_BYTES (5u << 20)

@@ -844,7 +844,7 @@ void fill_turns(float theta, int dh, u64* turn) {
   memcpy(turn, kept.turn, sizeof(u64) * (dh / 2));
 }
 
-// One item a thread while all blocks run at once (8 rows of 32 heads: 2.4 us, 2.9 with three), three beyond (8,000 rows of 32 / 8 heads in
+// One item a thread while all blocks run at once (8 rows of 32 heads: 2.4 us, 2.9 with three), three beyond (6,850 rows of 32 / 8 heads in
 // bf16: 30.0 us, 5.6 TB/s; 34.7 with one or two, 31.5 with four).
 template <typename TS, typename TD, int ITEMS>
 cudaError_t run_write_items(const WriteParams& p, int rows, int items, cudaStream_t st) {
