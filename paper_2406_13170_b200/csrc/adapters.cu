@@ -5,7 +5,7 @@
 //   y[r][s][o] = sum P + scale[i_r] sum_j t[r][s][j] b[i_r][s][o][j]  reduction of the partial sums, adapters' way back up (up)
 //
 // Small projections and those that the tensor-core kernels do not take: down, then all of y in one kernel (whole; fp32: the plain
-// projection's epilogue).
+// projection's epilogue).  A few rows: down and up in one kernel (few).
 #include <math.h>
 
 #include <mutex>
@@ -434,6 +434,135 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
   }
 }
 
+// adapter_down and adapter_up in one for a few rows (kFewRows) and a small rank: grid (128 columns, tile, segment), a block works out its
+// tile's t itself while the projection ahead still runs (which has started it once everything ahead of itself was done), holds b in registers,
+// waits, and adds the partial sums.  Its warps share K for t and have 16 columns each for y.  (One row of 4096 x 4096, rank 16: 9.3 us, 11.3
+// with the two kernels, and one launch less for the host.)
+constexpr int kFewRows = 16, kFewRank = 32;
+template <int QUADS, bool VEC, typename TY>
+__global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_constant__ AdapterArgs p, const PartialView P) {
+  constexpr int J = QUADS ? 8 : 4, NT = J / 2;                           // j of a lane; eights of the rank
+  __shared__ __align__(16) float red[kDownWarps][kTileRows][8 * NT + 4];
+  __shared__ __align__(16) bf16 t_hi[kTileRows][8 * NT], t_lo[kTileRows][8 * NT];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, seg = blockIdx.z;
+  // the tile: an adapter's rows, adapters in the order of their first rows; every warp finds it
+  const int mine = lane < p.rows ? adapter_of(p, lane) : -2;
+  const unsigned same = __match_any_sync(~0u, mine);
+  const unsigned firsts = __ballot_sync(~0u, mine != -2 && __ffs(same) - 1 == lane);
+  const int first = __fns(firsts, 0, blockIdx.y + 1);                     // lane of this tile's first row
+  if ((int)blockIdx.y >= __popc(firsts)) {
+    pdl_wait();
+    return;
+  }
+  const int adapter = __shfl_sync(~0u, mine, first);
+  const unsigned rows = __shfl_sync(~0u, same, first);
+  const int n = __popc(rows);
+  int row[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) row[i] = __fns(rows, 0, (g + 8 * i < n ? g + 8 * i : 0) + 1);
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  const int c0 = (blockIdx.x * kDownWarps + warp) * 16;
+  uint32_t hi[2][J / 2], lo[2][J / 2], b[2][J / 2];
+  if (adapter >= 0) {
+    const bf16* bs = (const bf16*)p.b + ((size_t)adapter * p.n_seg + seg) * p.out * p.rank;
+    const bool is = t * J < p.rank;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bf16* src = bs + (size_t)min(c0 + 4 * (g >> 1) + 2 * i + (g & 1), p.out - 1) * p.rank + (is ? t * J : 0);
+#pragma unroll
+      for (int k = 0; k < J / 2; k += 2) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(src + 2 * k));
+        b[i][k] = is ? u.x : 0u;
+        b[i][k + 1] = is ? u.y : 0u;
+      }
+    }
+    const bf16* a = (const bf16*)p.a + (((size_t)adapter * p.n_seg + seg) * p.rank) * p.in;
+    const int nt = p.rank / 8, steps = (p.in + 63) / 64;
+    float acc[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+#pragma unroll 2
+    for (int s = warp; s < steps; s += kDownWarps) {
+      uint4 xv[2][2], av[NT][2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int k = min(s * 64 + c * 32 + t * 8, p.in - 8);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xv[i][c] = __ldg(reinterpret_cast<const uint4*>((const bf16*)p.x + (size_t)row[i] * p.in + k));
+#pragma unroll
+        for (int j = 0; j < NT; ++j) av[j][c] = __ldg(reinterpret_cast<const uint4*>(a + (size_t)((j < nt ? j : 0) * 8 + g) * p.in + k));
+      }
+      if (s * 64 + 64 > p.in) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          if (s * 64 + c * 32 + t * 8 >= p.in) {
+            xv[0][c] = xv[1][c] = zero;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) av[j][c] = zero;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          mma_16816(acc[j], xv[0][c].x, xv[1][c].x, xv[0][c].y, xv[1][c].y, av[j][c].x, av[j][c].y);
+          mma_16816(acc[j], xv[0][c].z, xv[1][c].z, xv[0][c].w, xv[1][c].w, av[j][c].z, av[j][c].w);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      *reinterpret_cast<float2*>(&red[warp][g][j * 8 + 2 * t]) = make_float2(acc[j][0], acc[j][1]);
+      *reinterpret_cast<float2*>(&red[warp][g + 8][j * 8 + 2 * t]) = make_float2(acc[j][2], acc[j][3]);
+    }
+    __syncthreads();
+    const float scale = p.scale ? p.scale[adapter] : 1.f;
+    for (int i = tid; i < kTileRows * 8 * NT; i += kDownThreads) {
+      const int q = i / (8 * NT), j = i % (8 * NT);
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < kDownWarps; ++w) v += red[w][q][j];
+      halves(j < p.rank ? scale * v : 0.f, t_hi[q][j], t_lo[q][j]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int k = 0; k < J / 2; k += 2) {
+        const uint2 u = *reinterpret_cast<const uint2*>(&t_hi[g + 8 * i][t * J + 2 * k]), v = *reinterpret_cast<const uint2*>(&t_lo[g + 8 * i][t * J + 2 * k]);
+        hi[i][k] = u.x; hi[i][k + 1] = u.y;
+        lo[i][k] = v.x; lo[i][k + 1] = v.y;
+      }
+  }
+  pdl_wait();                                                             // the partial sums
+  pdl_launch_dependents();
+  const int col = c0 + 4 * t, left = p.out - col;
+  float4 sum[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+  const float* src[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) src[i] = P.p + (size_t)row[i] * P.ld + seg * p.out + (left > 0 ? col : 0);
+#pragma unroll 8
+  for (int s = 0; s < P.splits; ++s)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) add4(sum[i], get4<VEC>(src[i] + s * P.split_stride, left));
+  if (adapter >= 0) {
+    float acc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+#pragma unroll
+      for (int k = 0; k < J / 2; k += 2) {
+        mma_16816(acc[i], lo[0][k], lo[1][k], lo[0][k + 1], lo[1][k + 1], b[i][k], b[i][k + 1]);
+        mma_16816(acc[i], hi[0][k], hi[1][k], hi[0][k + 1], hi[1][k + 1], b[i][k], b[i][k + 1]);
+      }
+    }
+    add4(sum[0], make_float4(acc[0][0], acc[0][1], acc[1][0], acc[1][1]));
+    add4(sum[1], make_float4(acc[0][2], acc[0][3], acc[1][2], acc[1][3]));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (g + 8 * i < n && left > 0) put4<VEC>((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + col, sum[i], left);
+}
+
 // The whole of y behind adapter_down, for projections that are small or that the tensor-core kernels do not take: grid (32 columns, tile,
 // segment).  A block's warps share K, 64 of it at a time, and the rank, 32 of it at a time; both are terms of one sum of MMAs (rows as A,
 // weights or b as B, t in two halves), which meets in shared memory.  Every tile reads the weights again.  Bound: latency for small shapes,
@@ -590,6 +719,16 @@ cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaS
   return run_up<4, TY>(p, pv, tiles, st);
 }
 
+// Bytes of a that adapter_few's blocks may read in all (5 rows of as many adapters, 13824 x 5120, rank 24: 43 us with 130 MB, 26.3 with the two kernels; 12 rows,
+// 17 MB: 21.3 and 18.6; 16 rows, 11 MB: 19.4 and 19.5)
+constexpr int64_t kFewBytes = 16 << 20;
+template <int QUADS, typename TY>
+cudaError_t run_few(const AdapterArgs& p, const PartialView& pv, int tiles, cudaStream_t st) {
+  const dim3 grid((p.out + kDownWarps * 16 - 1) / (kDownWarps * 16), tiles, p.n_seg);
+  return p.out % 4 == 0 ? launch_pdl(adapter_few_kernel<QUADS, true, TY>, grid, dim3(kDownThreads), 0, st, p, pv)
+                        : launch_pdl(adapter_few_kernel<QUADS, false, TY>, grid, dim3(kDownThreads), 0, st, p, pv);
+}
+
 template <typename TY>
 cudaError_t run_whole(const AdapterArgs& p, const void* const* w, int tiles, cudaStream_t st) {
   Weights ws = {};
@@ -697,11 +836,16 @@ amph_status project_adapters(const void* x_dev, int32_t x_rows_cap, const void* 
     pv.splits = splits;
     pv.split_stride = stride;
   }
-  if (dtype == AMPH_DTYPE_F32)
+  const bool few = g && rows <= kFewRows && ad->rank <= kFewRank &&
+                   (int64_t)((out + 127) / 128) * tiles * n_seg * ad->rank * in * 2 <= kFewBytes;
+  if (few)
+    e = ad->rank <= 16 ? (y_dtype == AMPH_DTYPE_F32 ? run_few<0, float>(p, pv, tiles, st) : run_few<0, bf16>(p, pv, tiles, st))
+                       : (y_dtype == AMPH_DTYPE_F32 ? run_few<1, float>(p, pv, tiles, st) : run_few<1, bf16>(p, pv, tiles, st));
+  else if (dtype == AMPH_DTYPE_F32)
     e = launch_pdl(adapter_down_plain_kernel, dim3((cols + 3) / 4, rows), dim3(kThreads), 0, st, p);
   else
     e = run_down(p, tiles, col_blocks, st);
-  if (e == cudaSuccess) {
+  if (e == cudaSuccess && !few) {
     if (dtype == AMPH_DTYPE_F32)
       e = launch_plain_adapters(x_dev, w, n_seg, out, in, (float*)y_dev, rows, {p.t, (const float*)p.b, p.scale, row_adapter, p.n_adapters, p.rank}, st);
     else if (whole)

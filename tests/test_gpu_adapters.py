@@ -111,6 +111,9 @@ def test_values(rows, n_seg, out, in_, rank, n, tc, dtype):
 LARGE = [                                            # enough weights and rows for the tcgen05 kernels, odd tiles of both
     (1, 8, 1024, 2048, 8, 1, True),
     (5, 2, 2048, 2048, 16, 3, True),
+    (3, 1, 1024, 4096, 32, 2, True),                  # up to 16 rows of a small rank: sums and adapters in one kernel
+    (16, 1, 2048, 1408, 24, 4, True),
+    (9, 2, 4096, 1024, 8, 9, True),
     (17, 1, 4096, 1408, 128, 2, True),
     (64, 3, 2048, 1408, 64, 70, True),
     (70, 3, 768, 1024, 8, 4, True),
