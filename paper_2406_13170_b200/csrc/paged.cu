@@ -862,9 +862,10 @@ cudaError_t run_write(const WriteParams& p, int rows, cudaStream_t st) {
 
 // What the table has room for, up to which an item gets a cluster: keys of a block, bytes of all keys and values.  Captured, line / cluster: one
 // sequence of 640 tokens, 32 heads 9.0 / 6.1 us, 16 of 800 with 8 heads to one of 64 8.2 / 5.0, one of 2000 with 8 heads to one 14.0 / 6.0, of
-// 8000 16.7 / 13.0, of 30000 26 / 37; 33 MB (8 of 2000, 32 / 8 heads) 15.5 / 18.7.
+// 8000 16.7 / 13.0, of 30000 26 / 37; room for 33 MB (32 of 2000, 8 / 2 heads of 64) 11.6 / 8.1, 43 MB (two of 1300, 32 heads) 15.5 / 14.8, 65 MB
+// (8 of 2000, 32 / 8 heads) 15.5 / 18.6.
 constexpr int kShortKeys = 8 * kUnit;
-constexpr int64_t kShortBytes = 16 << 20;
+constexpr int64_t kShortBytes = 40 << 20;
 // Launches the kernel in clusters of `blocks`, or, with `active`, asks how many of them run at a time.
 cudaError_t launch_cluster(void (*kernel)(AttendParams), dim3 grid, int blocks, size_t smem, cudaStream_t st, const AttendParams& p, int* active = nullptr) {
   cudaLaunchConfig_t cfg = {};
