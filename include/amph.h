@@ -352,6 +352,7 @@ typedef struct {
  * x, w, n_seg, out, in, rows (1..512), x_rows_cap, dtype and use_tensor_core as for amph_project (small bf16 projections, and those with
  * use_tensor_core = 0, run on the warp-level tensor cores).  y: [rows][n_seg*out] of
  * y_dtype, 16-byte aligned (AMPH_DTYPE_F32, or AMPH_DTYPE_BF16 with bf16 weights: the sums, held in fp32, are rounded once).
+ * y must not overlap an input.
  * ws_dev: device scratch, 256-byte aligned, at least amph_project_adapters_bytes() bytes; nothing in it needs to be set and nothing
  * is kept in it.  Calls that may overlap on the GPU need scratch of their own.  Make the first call on a device outside a stream capture. */
 amph_status amph_project_adapters_bytes(int32_t n_seg, int32_t out, int32_t rows, int32_t rank, size_t* ws_bytes);
