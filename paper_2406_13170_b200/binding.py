@@ -533,6 +533,8 @@ class PagedCache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         if k_pages.dim() != 4 or k_pages.dtype not in _DTYPES:
             _refuse(2, f"k_pages must be [n_pages, n_kv_heads, page_size, head_dim], float32 or bfloat16 (got {tuple(k_pages.shape)}, {k_pages.dtype})")
+        if k_pages.shape[3] not in (64, 128):
+            _refuse(2, f"head_dim must be 64 or 128 (got {k_pages.shape[3]})")
         if not k_pages.is_cuda:
             _refuse(7, "pages must be on a CUDA device")
         self.device, self.dtype = k_pages.device, k_pages.dtype

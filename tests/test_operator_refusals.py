@@ -134,6 +134,16 @@ def test_python_entries_refuse_host_tensors():
     assert e.value.status == 7
 
 
+@pytest.mark.parametrize("head_dim", [0, 1, 32, 96, 256])
+def test_a_cache_of_other_head_sizes_cannot_be_made(head_dim):
+    """Refused before the device is looked at: paged_write counts q's heads by it."""
+    for dtype in (torch.float32, torch.bfloat16):
+        pages = torch.zeros(4, 2, 16, head_dim, dtype=dtype)
+        with pytest.raises(b.AmphError, match="head_dim") as e:
+            b.PagedCache(pages, pages.clone())
+        assert e.value.status == 2
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 7, 148, 444, 592])
 def test_units_spread_over_blocks(n):
     """Block c takes units [total c / n, total (c + 1) / n); block_of() of the attention kernel names the block of a unit."""
