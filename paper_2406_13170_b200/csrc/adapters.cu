@@ -44,7 +44,7 @@ struct AdapterArgs {
 
 // The row's adapter, -1 if it has none (or names one that does not exist, which is reported).
 __device__ __forceinline__ int adapter_of(const AdapterArgs& p, int row) {
-  const int a = p.row_adapter[row];
+  const int a = __ldcg(p.row_adapter + row);
   if (a < p.n_adapters) return a < 0 ? -1 : a;
   if (p.status != nullptr) *p.status = AMPH_ERR_INVALID_ARG;
   return -1;
@@ -189,8 +189,8 @@ __device__ __forceinline__ void halves(float v, bf16& hi, bf16& lo) {
 // contiguous bytes for two steps.  The warps take turns at 64 columns of k and meet in shared memory, the ranges in that of the cluster's
 // first block; what leaves is scale * t as two bf16 halves (2^-17 of the adapter's share), the way adapter_up's MMA takes it.
 // `beside`: the kernel ahead is the tensor-core projection, which starts this one once everything ahead of itself is done, so it takes
-// the SMs and the shared memory that the projection leaves; only the first block waits for the projection, so that both are done when
-// this one is.  (Ahead of the projection, q / k / v of 64 rows of 24
+// the SMs and the shared memory that the projection leaves; what it reads is older than the projection (and past L1, see pdl_wait); only the first block
+// waits for the projection, so that both are done when this one is.  (Ahead of the projection, q / k / v of 64 rows of 24
 // tenants took 36.1 us in all, 28.0 now; gate / up of 37 rows at rank 64 48.5, 44.2 now; 512 rows, see down_splits, 59 and 47.9.)  72 registers:
 // beside a CTA of the pair kernel an SM's schedulers have room for two such warps each, not for two of 80.
 // Bound: latency for a few rows, the adapters' bytes for many tenants.
@@ -232,10 +232,10 @@ __global__ void __maxnreg__(72) adapter_down_kernel(const AdapterArgs p) {
       for (int c = 0; c < 2; ++c) {
         const int k = s * 64 + c * 32 + t * 8;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) xv[i][c] = x[i] != nullptr && k < p.in ? __ldg(reinterpret_cast<const uint4*>(x[i] + k)) : zero;
+        for (int i = 0; i < 2; ++i) xv[i][c] = x[i] != nullptr && k < p.in ? __ldcg(reinterpret_cast<const uint4*>(x[i] + k)) : zero;
 #pragma unroll
         for (int j = 0; j < kDownCols / 8; ++j)
-          av[j][c] = j < nt && k < p.in ? __ldg(reinterpret_cast<const uint4*>(a + (size_t)j * 8 * p.in + k)) : zero;
+          av[j][c] = j < nt && k < p.in ? __ldcg(reinterpret_cast<const uint4*>(a + (size_t)j * 8 * p.in + k)) : zero;
       }
 #pragma unroll
       for (int j = 0; j < kDownCols / 8; ++j)
@@ -287,7 +287,7 @@ __global__ void __maxnreg__(72) adapter_down_kernel(const AdapterArgs p) {
     if (waits) pdl_wait();
     return;
   }
-  const float scale = p.scale ? p.scale[tile.adapter] : 1.f;
+  const float scale = p.scale ? __ldcg(p.scale + tile.adapter) : 1.f;
 #pragma unroll
   for (int q = 0; q < kTileRows * kDownCols / kDownThreads; ++q) {
     const int i = q * kDownThreads + tid, r = i / width, c = i - r * width;
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
 }
 
 // adapter_down and adapter_up in one for a few rows (kFewRows) and a small rank: grid (128 columns, tile, segment), a block works out its
-// tile's t itself while the projection ahead still runs (which has started it once everything ahead of itself was done), holds b in registers,
+// tile's t itself while the projection ahead still runs (which has started it once everything ahead of itself was done, see pdl_wait), holds b in registers,
 // waits, and adds the partial sums.  Its warps share K for t and have 16 columns each for y.  (One row of 4096 x 4096, rank 16: 9.3 us, 11.3
 // with the two kernels, and one launch less for the host.)
 constexpr int kFewRows = 16, kFewRank = 32;
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
       const bf16* src = bs + (size_t)min(c0 + 4 * (g >> 1) + 2 * i + (g & 1), p.out - 1) * p.rank + (is ? t * J : 0);
 #pragma unroll
       for (int k = 0; k < J / 2; k += 2) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(src + 2 * k));
+        const uint2 u = __ldcg(reinterpret_cast<const uint2*>(src + 2 * k));
         b[i][k] = is ? u.x : 0u;
         b[i][k + 1] = is ? u.y : 0u;
       }
@@ -488,9 +488,9 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
       for (int c = 0; c < 2; ++c) {
         const int k = min(s * 64 + c * 32 + t * 8, p.in - 8);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) xv[i][c] = __ldg(reinterpret_cast<const uint4*>((const bf16*)p.x + (size_t)row[i] * p.in + k));
+        for (int i = 0; i < 2; ++i) xv[i][c] = __ldcg(reinterpret_cast<const uint4*>((const bf16*)p.x + (size_t)row[i] * p.in + k));
 #pragma unroll
-        for (int j = 0; j < NT; ++j) av[j][c] = __ldg(reinterpret_cast<const uint4*>(a + (size_t)((j < nt ? j : 0) * 8 + g) * p.in + k));
+        for (int j = 0; j < NT; ++j) av[j][c] = __ldcg(reinterpret_cast<const uint4*>(a + (size_t)((j < nt ? j : 0) * 8 + g) * p.in + k));
       }
       if (s * 64 + 64 > p.in) {
 #pragma unroll
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
       *reinterpret_cast<float2*>(&red[warp][g + 8][j * 8 + 2 * t]) = make_float2(acc[j][2], acc[j][3]);
     }
     __syncthreads();
-    const float scale = p.scale ? p.scale[adapter] : 1.f;
+    const float scale = p.scale ? __ldcg(p.scale + adapter) : 1.f;
     for (int i = tid; i < kTileRows * 8 * NT; i += kDownThreads) {
       const int q = i / (8 * NT), j = i % (8 * NT);
       float v = 0.f;

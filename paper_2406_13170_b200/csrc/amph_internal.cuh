@@ -66,6 +66,9 @@ struct DevState {
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// What kernels AHEAD of the predecessor wrote may be read without pdl_wait() where every block of the predecessor triggers behind its own
+// pdl_wait(): those kernels have ended then, with their writes in L2, before this one starts.  What an SM's L1 holds may be older, since
+// pdl_wait() is what promises a fresh view, so such reads go past it: ld.global.cg (__ldcg).
 
 template <typename... P, typename... A>
 inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args) {

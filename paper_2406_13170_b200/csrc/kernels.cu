@@ -733,7 +733,10 @@ gemm_generic_kernel(const T* __restrict__ X, int ldx, const __grid_constant__ Ge
       for (int v = 0; v < 2; ++v) {
         const int k = c * KC + (v * 32 + lane) * V;
         w[i][v] = make_uint4(0u, 0u, 0u, 0u);
-        if (o0 + i * step < out && k < in) w[i][v] = *reinterpret_cast<const uint4*>(weights(i) + (size_t)(o0 + i * step) * in + k);
+        if (o0 + i * step < out && k < in) {
+          const uint4* src = reinterpret_cast<const uint4*>(weights(i) + (size_t)(o0 + i * step) * in + k);
+          w[i][v] = EPI == PLAIN_ADAPT ? __ldcg(src) : *src;       // ADAPT: weights may be an earlier call's output (see pdl_wait)
+        }
       }
   };
   auto load_x = [&](int c) {
