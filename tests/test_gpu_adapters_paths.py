@@ -187,3 +187,83 @@ def test_an_attention_s_output_is_the_next_projection_s_rows():
         got = [step(i, False) for i in range(24)]
         torch.cuda.synchronize()
         assert all(torch.equal(y, want[i % 3]) for i, y in enumerate(got))
+
+
+@paths
+@pytest.mark.parametrize("which", ["mixed", "runs", "one", "none"])
+def test_rows_of_every_kind(path, which):
+    """Rows behind the last, adapters that no row names and the scratch hold NaN and infinities; rows of y behind the last are left alone."""
+    c = Call(path, seed=2)
+    c.x[c.rows:] = float("nan")
+    spare = c.n - 1                                    # named by no row
+    rows = torch.arange(c.rows, device=DEV)
+    c.at.copy_({"mixed": (rows * 7 + rows // 3) % (spare + 1) - 1, "runs": rows * spare // c.rows, "one": rows * 0 + spare - 1, "none": rows * 0 - 1}[which])
+    want = c.want()
+    c.a[spare], c.b[spare], c.scale[spare] = float("nan"), float("inf"), float("nan")
+    junk = [torch.full((1 << 24,), float("nan"), device=DEV) for _ in range(4)]
+    del junk                                           # the scratch is likely to be one of these
+    buf = torch.full((c.rows + 3, c.n_seg * c.out), 7.0, device=DEV)
+    c.run(y=buf[: c.rows])
+    assert torch.equal(buf[: c.rows], want) and bool((buf[c.rows:] == 7.0).all())
+
+
+@paths
+def test_a_row_s_own_nan_is_its_own(path):
+    c = Call(path, seed=3)
+    c.at.copy_(torch.arange(c.rows, device=DEV) % c.n)
+    y = c.run()
+    c.x[1, 5] = float("nan")
+    z = c.run()
+    others = torch.arange(c.rows, device=DEV) != 1
+    assert torch.isnan(z[1]).all() and torch.equal(z[others], y[others])
+    c.x[1, 5] = 0
+    mine, theirs = (c.at == 0), (c.at != 0)
+    y = c.run()
+    c.a[0, 0, 3, 7] = float("nan")
+    z = c.run()
+    assert torch.isnan(z[mine][:, : c.out]).all() and torch.equal(z[theirs], y[theirs]) and torch.equal(z[:, c.out:], y[:, c.out:])
+
+
+@paths
+def test_adapters_that_do_not_exist(path):
+    c = Call(path, seed=4)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for wrong in (c.n, 2 ** 31 - 1):
+        for row in (0, c.rows // 2, c.rows - 1):
+            at = (torch.arange(c.rows, device=DEV, dtype=torch.int32) % (c.n + 1) - 1)
+            at[row] = wrong
+            c.at.copy_(at)
+            y = c.run(status=status.zero_())
+            assert int(status) == 1
+            c.at[row] = -1
+            assert torch.equal(y, c.want())
+            assert torch.equal(c.run(status=status.zero_()), y) and int(status) == 0
+
+
+@paths
+def test_replays_with_other_inputs(path):
+    c = Call(path, seed=5)
+    c.run()
+    gr = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(gr):
+        y = c.run()
+    for _ in range(3):
+        for old, new in zip((c.x, *c.w, c.a, c.b, c.scale, c.at), (lambda x, w, *rest: (x, *w, *rest))(*c.inputs())):
+            old.copy_(new)
+        gr.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, c.want())
+
+
+@pytest.mark.parametrize("path", [p for p in PATHS if p != "fp32"])
+def test_infinite_weights_of_an_adapter(path):
+    """b = inf: where the low-rank product is not zero the sum is infinite or NaN (its two bf16 halves may differ in sign), elsewhere as without it."""
+    c = Call(path, seed=6)
+    c.at.copy_(torch.arange(c.rows, device=DEV) % c.n)
+    y = c.run()
+    c.b[0, 0, 9, 2] = float("inf")
+    z = c.run()
+    hit = torch.zeros_like(y, dtype=torch.bool)
+    hit[c.at == 0, 9] = True
+    assert not torch.isfinite(z[hit]).any() and torch.equal(z[~hit], y[~hit])
