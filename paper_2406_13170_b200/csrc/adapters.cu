@@ -21,7 +21,6 @@ typedef __nv_bfloat16 bf16;
 constexpr int kMaxRowsAll = 4 * kMaxRows;
 constexpr int kThreads = 128;
 
-
 // Up to kTileRows rows of one adapter (or without any: adapter < 0), as adapter_down leaves them for adapter_up.
 constexpr int kTileRows = 16;
 struct __align__(16) RowTile {
@@ -308,16 +307,12 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ void add4(float4& a, const float4 v) { a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
-// four values, or the first `left` of them
-template <bool VEC>
-__device__ __forceinline__ float4 get4(const float* p, int left) {
-  if constexpr (VEC) return *reinterpret_cast<const float4*>(p);
-  return make_float4(p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
-}
+__device__ __forceinline__ float4 get4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put_all(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void put_all(bf16* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack(v.x, v.y), pack(v.z, v.w)); }
+// four values (VEC), or the first `left` of them
 template <bool VEC, typename TY>
 __device__ __forceinline__ void put4(TY* p, float4 v, int left) {
   if constexpr (VEC) { put_all(p, v); return; }
@@ -331,9 +326,10 @@ __device__ __forceinline__ void put4(TY* p, float4 v, int left) {
 // columns of the tile's rows at a time.  MMA with t's halves as A and b as B.  As in adapter_down the sum over j may run in any order: a
 // lane takes four (rank up to 16: QUADS = 0) or eight neighbouring j, QUADS is how many times 32 of them.  A lane's two output tiles are
 // numbered so that it owns four neighbouring columns.  A lane without a row reads row 0's sums, unconditionally (loads behind a branch are
-// waited for one by one: 7.4 us instead of 3.6 for one row of 4096), and writes nothing.  VEC: out is a multiple of four.  Bound: L2 (partial sums) and the bytes of b and y.
+// waited for one by one: 7.4 us instead of 3.6 for one row of 4096), and writes nothing.  out is a multiple of 128 (as the projection wants it),
+// so a warp's columns are there or not as a whole.  Bound: L2 (partial sums) and the bytes of b and y.
 __host__ __device__ constexpr int up_groups(int quads) { return quads <= 2 ? 2 : 1; }        // 16 columns each, whose loads are in flight together
-template <int QUADS, bool VEC, typename TY>
+template <int QUADS, typename TY>
 __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs p, const PartialView P, int steps) {
   pdl_wait();
   pdl_launch_dependents();
@@ -382,7 +378,7 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
 #pragma unroll
           for (int c = 0; c < CHUNKS; ++c) {
             const int j = (c * 4 + t) * J;
-            load_j(b + (size_t)o * p.rank + j, o < p.out && j < p.rank, bv[q][i][c]);
+            load_j(b + (size_t)o * p.rank + j, j < p.rank, bv[q][i][c]);
           }
         }
     }
@@ -395,16 +391,13 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
 #pragma unroll
     for (int q = 0; q < GROUPS; ++q)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int col = c0 + q * 16 + 4 * t;
-        src[q][i] = P.p + (size_t)max(row[i], 0) * P.ld + seg * p.out + (col < p.out ? col : 0);
-      }
+      for (int i = 0; i < 2; ++i) src[q][i] = P.p + (size_t)max(row[i], 0) * P.ld + seg * p.out + c0 + q * 16 + 4 * t;
 #pragma unroll 4
     for (int s = 0; s < P.splits; ++s)
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) add4(sum[q][i], get4<VEC>(src[q][i] + s * P.split_stride, p.out - (c0 + q * 16 + 4 * t)));
+        for (int i = 0; i < 2; ++i) add4(sum[q][i], get4(src[q][i] + s * P.split_stride));
     if (adapter >= 0) {
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q) {
@@ -427,10 +420,8 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
 #pragma unroll
     for (int q = 0; q < GROUPS; ++q)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int col = c0 + q * 16 + 4 * t;
-        if (row[i] >= 0 && col < p.out) put4<VEC>((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + col, sum[q][i], p.out - col);
-      }
+      for (int i = 0; i < 2; ++i)
+        if (row[i] >= 0) put_all((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + c0 + q * 16 + 4 * t, sum[q][i]);
   }
 }
 
@@ -439,7 +430,7 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
 // waits, and adds the partial sums.  Its warps share K for t and have 16 columns each for y.  (One row of 4096 x 4096, rank 16: 9.3 us, 11.3
 // with the two kernels, and one launch less for the host.)
 constexpr int kFewRows = 16, kFewRank = 32;
-template <int QUADS, bool VEC, typename TY>
+template <int QUADS, typename TY>
 __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_constant__ AdapterArgs p, const PartialView P) {
   constexpr int J = QUADS ? 8 : 4, NT = J / 2;                           // j of a lane; eights of the rank
   __shared__ __align__(16) float red[kDownWarps][kTileRows][8 * NT + 4];
@@ -460,7 +451,6 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
   int row[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) row[i] = __fns(rows, 0, (g + 8 * i < n ? g + 8 * i : 0) + 1);
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
   const int c0 = (blockIdx.x * kDownWarps + warp) * 16;
   uint32_t hi[2][J / 2], lo[2][J / 2], b[2][J / 2];
   if (adapter >= 0) {
@@ -468,7 +458,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
     const bool is = t * J < p.rank;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const bf16* src = bs + (size_t)min(c0 + 4 * (g >> 1) + 2 * i + (g & 1), p.out - 1) * p.rank + (is ? t * J : 0);
+      const bf16* src = bs + (size_t)(c0 + 4 * (g >> 1) + 2 * i + (g & 1)) * p.rank + (is ? t * J : 0);
 #pragma unroll
       for (int k = 0; k < J / 2; k += 2) {
         const uint2 u = __ldcg(reinterpret_cast<const uint2*>(src + 2 * k));
@@ -477,7 +467,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
       }
     }
     const bf16* a = (const bf16*)p.a + (((size_t)adapter * p.n_seg + seg) * p.rank) * p.in;
-    const int nt = p.rank / 8, steps = (p.in + 63) / 64;
+    const int nt = p.rank / 8, steps = p.in / 64;
     float acc[NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
@@ -486,20 +476,11 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
       uint4 xv[2][2], av[NT][2];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int k = min(s * 64 + c * 32 + t * 8, p.in - 8);
+        const int k = s * 64 + c * 32 + t * 8;
 #pragma unroll
         for (int i = 0; i < 2; ++i) xv[i][c] = __ldcg(reinterpret_cast<const uint4*>((const bf16*)p.x + (size_t)row[i] * p.in + k));
 #pragma unroll
         for (int j = 0; j < NT; ++j) av[j][c] = __ldcg(reinterpret_cast<const uint4*>(a + (size_t)((j < nt ? j : 0) * 8 + g) * p.in + k));
-      }
-      if (s * 64 + 64 > p.in) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-          if (s * 64 + c * 32 + t * 8 >= p.in) {
-            xv[0][c] = xv[1][c] = zero;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) av[j][c] = zero;
-          }
       }
 #pragma unroll
       for (int j = 0; j < NT; ++j)
@@ -535,15 +516,15 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
   }
   pdl_wait();                                                             // the partial sums
   pdl_launch_dependents();
-  const int col = c0 + 4 * t, left = p.out - col;
+  const int col = c0 + 4 * t;
   float4 sum[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
   const float* src[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) src[i] = P.p + (size_t)row[i] * P.ld + seg * p.out + (left > 0 ? col : 0);
+  for (int i = 0; i < 2; ++i) src[i] = P.p + (size_t)row[i] * P.ld + seg * p.out + col;
 #pragma unroll 8
   for (int s = 0; s < P.splits; ++s)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) add4(sum[i], get4<VEC>(src[i] + s * P.split_stride, left));
+    for (int i = 0; i < 2; ++i) add4(sum[i], get4(src[i] + s * P.split_stride));
   if (adapter >= 0) {
     float acc[2][4];
 #pragma unroll
@@ -560,7 +541,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_few_kernel(const __grid_
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    if (g + 8 * i < n && left > 0) put4<VEC>((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + col, sum[i], left);
+    if (g + 8 * i < n) put_all((TY*)p.y + (size_t)row[i] * P.ld + seg * p.out + col, sum[i]);
 }
 
 // The whole of y behind adapter_down, for projections that are small or that the tensor-core kernels do not take: grid (32 columns, tile,
@@ -708,8 +689,7 @@ cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaS
   int steps = (int)((int64_t)blocks * tiles * p.n_seg / (148 * 8));
   steps = steps < 1 ? 1 : (steps > 4 ? 4 : steps);
   const dim3 grid((blocks + steps - 1) / steps, tiles, p.n_seg);
-  return p.out % 4 == 0 ? launch_pdl(adapter_up_kernel<QUADS, true, TY>, grid, dim3(kThreads), 0, st, p, pv, steps)
-                        : launch_pdl(adapter_up_kernel<QUADS, false, TY>, grid, dim3(kThreads), 0, st, p, pv, steps);
+  return launch_pdl(adapter_up_kernel<QUADS, TY>, grid, dim3(kThreads), 0, st, p, pv, steps);
 }
 template <typename TY>
 cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaStream_t st) {
@@ -724,9 +704,8 @@ cudaError_t run_up(const AdapterArgs& p, const PartialView& pv, int tiles, cudaS
 constexpr int64_t kFewBytes = 16 << 20;
 template <int QUADS, typename TY>
 cudaError_t run_few(const AdapterArgs& p, const PartialView& pv, int tiles, cudaStream_t st) {
-  const dim3 grid((p.out + kDownWarps * 16 - 1) / (kDownWarps * 16), tiles, p.n_seg);
-  return p.out % 4 == 0 ? launch_pdl(adapter_few_kernel<QUADS, true, TY>, grid, dim3(kDownThreads), 0, st, p, pv)
-                        : launch_pdl(adapter_few_kernel<QUADS, false, TY>, grid, dim3(kDownThreads), 0, st, p, pv);
+  static_assert(kDownWarps * 16 == 128, "out is a multiple of a block's columns");
+  return launch_pdl(adapter_few_kernel<QUADS, TY>, dim3(p.out / 128, tiles, p.n_seg), dim3(kDownThreads), 0, st, p, pv);
 }
 
 template <typename TY>
