@@ -16,11 +16,10 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <array>
 #include <map>
 #include <optional>
-#include <tuple>
 #include <unordered_map>
+#include <utility>
 
 #include "amph.h"
 
@@ -69,29 +68,28 @@ T* held(PyObject* o, const char* name) {
   return (T*)PyCapsule_GetPointer(o, name);
 }
 
-// Scratch of a call of `kind` on a stream; `clean`: only calls of this kind have used it, all of them succeeded.  Calls on one stream follow one
-// another, so a stream keeps one piece per kind.  Calls that are captured share a piece per capture and stream, from the graph's memory:
-// graphs may be replayed beside one another and beside anything else, and what a replay finds is what its own first call sets.
-enum { FOR_ADAPTERS = 0, FOR_ATTENTION = 1 };
+// Scratch of an attention call on a stream, kept there since its counters are zero between calls (`clean`: only these calls have used it, all
+// of them succeeded), 5 MB.  Calls on one stream follow one another, so a stream has one piece.  Calls of one capture share a piece per stream, from the graph's memory: graphs may be replayed
+// beside one another and beside anything else, and what a replay finds is what its own first call sets.  It is given back once a call that is not
+// of that capture is made; a capture that still goes on then makes another.  (The other operators' scratch holds nothing between calls: an
+// ordinary temporary of the allocator's.)
 struct Scratch {
   at::Tensor t;
-  unsigned long long capture = 0;
   bool clean = false;
 };
-Scratch& scratch(int kind, int device, cudaStream_t stream, size_t need) {
-  static auto& eager = *new std::map<std::tuple<int, int, cudaStream_t>, Scratch>;       // never destroyed: the device may be gone by then
-  static auto& captured = *new std::map<std::tuple<int, int, cudaStream_t>, Scratch>;
+Scratch& attention_scratch(int device, cudaStream_t stream) {
+  typedef std::map<std::pair<int, cudaStream_t>, Scratch> Pieces;
+  static auto& eager = *new Pieces;                      // never destroyed: the device may be gone by then
+  static auto& captured = *new Pieces;
+  static unsigned long long capture = 0;                 // that `captured` belongs to
   cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
   unsigned long long id = 0;
   C10_CUDA_CHECK(cudaStreamGetCaptureInfo(stream, &status, &id));
-  Scratch& s = (status == cudaStreamCaptureStatusNone ? eager : captured)[{kind, device, stream}];
-  if (status == cudaStreamCaptureStatusNone) id = 0;
-  if (!s.t.defined() || s.capture != id || (size_t)s.t.numel() < need) {
-    s.t = at::Tensor();
-    s.clean = false;
-    s.capture = id;
-    s.t = make({(int64_t)need}, at::kByte, device);
-  }
+  const bool capturing = status != cudaStreamCaptureStatusNone;
+  if (!captured.empty() && (!capturing || id != capture)) captured.clear();
+  if (capturing) capture = id;
+  Scratch& s = (capturing ? captured : eager)[{device, stream}];
+  if (!s.t.defined()) s.t = make({AMPH_PAGED_WS_BYTES}, at::kByte, device);
   return s;
 }
 
@@ -181,9 +179,9 @@ PyObject* project_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   const at::Tensor y = y_in ? *y_in : make({(int64_t)rows, ld}, y_type, ad->device);
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)ad->device).stream();
-  Scratch& ws = scratch(FOR_ADAPTERS, ad->device, stream, need);
+  const at::Tensor ws = make({(int64_t)need}, at::kByte, ad->device);
   return give(y, lib.project_adapters(x->data_ptr(), (int)x->size(0), w, ad->n_seg, ad->out, ad->in, (int)rows, ad->dtype, tc, &ad->c,
-                                      (const int32_t*)at_->data_ptr(), y.data_ptr(), amph_dtype(y_type), ws.t.data_ptr(), need,
+                                      (const int32_t*)at_->data_ptr(), y.data_ptr(), amph_dtype(y_type), ws.data_ptr(), need,
                                       status ? (int32_t*)status->data_ptr() : nullptr, stream));
   END_HANDLE_TH_ERRORS
 }
@@ -258,7 +256,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor out = out_in ? *out_in : make(q->sizes(), type, dev);
   if (seqs == 0) return give(out, AMPH_OK);              // (an empty tensor has no address)
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
-  Scratch& ws = scratch(FOR_ATTENTION, dev, stream, AMPH_PAGED_WS_BYTES);
+  Scratch& ws = attention_scratch(dev, stream);
   const int rc = lib.paged_attention(&c->c, q->data_ptr(), (int)heads, (const int32_t*)lens->data_ptr(), (const int32_t*)table->data_ptr(), (int)seqs,
                                      (int)table->size(1), (float)scale, out.data_ptr(), lse ? (float*)lse->data_ptr() : nullptr, ws.t.data_ptr(),
                                      AMPH_PAGED_WS_BYTES, ws.clean, status ? (int32_t*)status->data_ptr() : nullptr, stream);
