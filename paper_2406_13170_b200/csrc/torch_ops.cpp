@@ -69,12 +69,14 @@ T* held(PyObject* o, const char* name) {
 }
 
 // Scratch of an attention call on a stream, kept there since its counters are zero between calls (`clean`: only these calls have used it, all
-// of them succeeded), 5 MB.  Calls on one stream follow one another, so a stream has one piece.  Calls of one capture share a piece per stream, from the graph's memory: graphs may be replayed
+// of them succeeded), 5 MB.  Calls on one stream follow one another, so a stream has one piece; a stream that was destroyed and another that got
+// its handle are told apart by their ids.  Calls of one capture share a piece per stream, from the graph's memory: graphs may be replayed
 // beside one another and beside anything else, and what a replay finds is what its own first call sets.  It is given back once a call that is not
 // of that capture is made; a capture that still goes on then makes another.  (The other operators' scratch holds nothing between calls: an
 // ordinary temporary of the allocator's.)
 struct Scratch {
   at::Tensor t;
+  unsigned long long stream_id = 0;
   bool clean = false;
 };
 Scratch& attention_scratch(int device, cudaStream_t stream) {
@@ -83,13 +85,18 @@ Scratch& attention_scratch(int device, cudaStream_t stream) {
   static auto& captured = *new Pieces;
   static unsigned long long capture = 0;                 // that `captured` belongs to
   cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-  unsigned long long id = 0;
+  unsigned long long id = 0, stream_id = 0;
   C10_CUDA_CHECK(cudaStreamGetCaptureInfo(stream, &status, &id));
   const bool capturing = status != cudaStreamCaptureStatusNone;
   if (!captured.empty() && (!capturing || id != capture)) captured.clear();
   if (capturing) capture = id;
+  else C10_CUDA_CHECK(cudaStreamGetId(stream, &stream_id));       // (not while it is captured)
   Scratch& s = (capturing ? captured : eager)[{device, stream}];
-  if (!s.t.defined()) s.t = make({AMPH_PAGED_WS_BYTES}, at::kByte, device);
+  if (!s.t.defined() || s.stream_id != stream_id) {
+    s.clean = false;
+    s.t = make({AMPH_PAGED_WS_BYTES}, at::kByte, device);         // (before the old one is given back: it may still be in use)
+    s.stream_id = stream_id;
+  }
   return s;
 }
 

@@ -1,4 +1,5 @@
 """What the operators for many requests keep on the device between calls, and for whom."""
+import ctypes as C
 import gc
 
 import pytest
@@ -86,3 +87,38 @@ def test_calls_outside_a_capture_that_goes_on():
             eager.append(paged_attention(*s))
         torch.cuda.synchronize()
         assert all(torch.equal(o, want) for o in y + eager)
+
+
+def test_a_stream_with_another_s_handle_gets_scratch_of_its_own():
+    """A stream is destroyed and the next one has its handle: work of the first may still run, so nothing of its scratch is taken over."""
+    from paper_2406_13170_b200 import paged_attention
+    s = _setup(73, lens=LONG[0])
+    want = paged_attention(*s)
+    out = torch.zeros_like(want)
+    rt = torch.cuda.cudart()
+    seen, came_back = set(), 0
+    for _ in range(4):
+        handles = []
+        for _ in range(20):
+            h = C.c_void_p()
+            assert int(rt.cudaStreamCreate(C.addressof(h))) == 0
+            handles.append(h.value)
+        made = []
+        for h in handles:
+            stream = torch.cuda.ExternalStream(h)
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                counts = [torch.cuda.memory_stats()["allocation.all.allocated"]]
+                for _ in range(2):
+                    paged_attention(*s, out=out)
+                    counts.append(torch.cuda.memory_stats()["allocation.all.allocated"])
+            stream.synchronize()
+            assert torch.equal(out, want)
+            made.append([b - a for a, b in zip(counts, counts[1:])])
+        came_back += len(seen & set(handles))
+        seen |= set(handles)
+        for h in handles:
+            assert int(rt.cudaStreamDestroy(h)) == 0
+        assert made == [[1, 0]] * len(handles)         # a new stream's first call makes scratch, its next one finds it
+    if not came_back:
+        pytest.skip("no handle came back")
