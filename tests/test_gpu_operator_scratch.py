@@ -64,29 +64,31 @@ def test_paged_attention_gives_a_capture_s_scratch_back():
         assert _allocated() == before
 
 
-def test_calls_outside_a_capture_that_goes_on():
+@pytest.mark.parametrize("mode", ["global", "thread_local", "relaxed"])
+def test_calls_outside_a_capture_that_goes_on(mode):
     """A capture on one stream, with calls outside it on another between its own."""
     from paper_2406_13170_b200 import paged_attention
     s = _setup(72, lens=LONG[1])
     want = paged_attention(*s)
     side, inside = torch.cuda.Stream(), torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
+    eager = [torch.zeros_like(want) for _ in range(6)]
     with torch.cuda.stream(side):
-        paged_attention(*s)
+        paged_attention(*s, out=eager[0])
     torch.cuda.synchronize()
     gr = torch.cuda.CUDAGraph()
-    y, eager = [], []
-    with torch.cuda.graph(gr, stream=inside, capture_error_mode="relaxed"):
-        for _ in range(3):
+    y = []
+    with torch.cuda.graph(gr, stream=inside, capture_error_mode=mode):
+        for i in range(3):
             y.append(paged_attention(*s))
             with torch.cuda.stream(side):
-                eager.append(paged_attention(*s))
-    for _ in range(3):
+                paged_attention(*s, out=eager[i])
+    for i in range(3):
         gr.replay()
         with torch.cuda.stream(side):
-            eager.append(paged_attention(*s))
+            paged_attention(*s, out=eager[3 + i])
         torch.cuda.synchronize()
-        assert all(torch.equal(o, want) for o in y + eager)
+        assert all(torch.equal(o, want) for o in y + eager[: 4 + i])
 
 
 def test_a_stream_with_another_s_handle_gets_scratch_of_its_own():
