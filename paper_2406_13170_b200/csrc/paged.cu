@@ -983,6 +983,8 @@ amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, i
   if (n_heads < 1 || n_heads > 1024 || n_heads % cache->n_kv_heads)
     return api_fail(AMPH_ERR_SHAPE, "n_heads (%d) must be a multiple of n_kv_heads (%d), at most 1024", n_heads, cache->n_kv_heads);
   if (n_seqs > AMPH_PAGED_MAX_SEQS) return api_fail(AMPH_ERR_SHAPE, "n_seqs must be at most %d (got %d)", AMPH_PAGED_MAX_SEQS, n_seqs);
+  const uintptr_t q_at = (uintptr_t)q, out_at = (uintptr_t)out, bytes = (uintptr_t)n_seqs * n_heads * cache->head_dim * (cache->dtype == AMPH_DTYPE_F32 ? 4 : 2);
+  if (q_at < out_at + bytes && out_at < q_at + bytes) return api_fail(AMPH_ERR_INVALID_ARG, "out must not overlap q");
   if (!isfinite(scale)) return api_fail(AMPH_ERR_INVALID_ARG, "scale must be finite");
   if (!aligned16(q) || !aligned16(out)) return api_fail(AMPH_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   if (!ws_dev || ((uintptr_t)ws_dev & 255) || ws_bytes < AMPH_PAGED_WS_BYTES)

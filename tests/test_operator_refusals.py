@@ -59,6 +59,19 @@ def test_attention_refuses(L, fault, status):
     assert _message(L)
 
 
+@pytest.mark.parametrize("dtype,bytes_", [(1, 2), (0, 4)])
+@pytest.mark.parametrize("n_seqs", [1, 3, 4096])
+def test_attention_refuses_an_output_that_overlaps_its_queries(L, n_seqs, dtype, bytes_):
+    """Rows of one sequence are written while another's are still read."""
+    size = n_seqs * 8 * 128 * bytes_
+    far = 1 << 32
+    for by in (16, size // 2, size - 16):
+        for out in (far + by, far - by):
+            assert _attend(L, _cache(dtype=dtype), q=far, out=out, n_seqs=n_seqs) == 1 and "overlap" in _message(L)
+    for out in (far + size, far - size):
+        assert _attend(L, _cache(dtype=dtype), q=far, out=out, n_seqs=n_seqs, ws=None) == 5       # (refused for another reason: no launch)
+
+
 def test_null_cache_and_empty_batches(L):
     assert L.amph_paged_attention(None, P, 8, P, P, 3, 4, 0.0, 2 * P, None, P, b.AMPH_PAGED_WS_BYTES, 0, None, None) == 1
     assert _attend(L, n_seqs=0) == 0                  # nothing to do: no launch
