@@ -985,7 +985,8 @@ amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, i
   if (n_seqs > AMPH_PAGED_MAX_SEQS) return api_fail(AMPH_ERR_SHAPE, "n_seqs must be at most %d (got %d)", AMPH_PAGED_MAX_SEQS, n_seqs);
   const uintptr_t q_at = (uintptr_t)q, out_at = (uintptr_t)out, bytes = (uintptr_t)n_seqs * n_heads * cache->head_dim * (cache->dtype == AMPH_DTYPE_F32 ? 4 : 2);
   if (q_at < out_at + bytes && out_at < q_at + bytes) return api_fail(AMPH_ERR_INVALID_ARG, "out must not overlap q");
-  if (!isfinite(scale)) return api_fail(AMPH_ERR_INVALID_ARG, "scale must be finite");
+  const float scale_log2 = (scale == 0.f ? 1.0f / sqrtf((float)cache->head_dim) : scale) * kLog2e;
+  if (!isfinite(scale_log2)) return api_fail(AMPH_ERR_INVALID_ARG, "scale must be finite, also times log2(e)");
   if (!aligned16(q) || !aligned16(out)) return api_fail(AMPH_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
   if (!ws_dev || ((uintptr_t)ws_dev & 255) || ws_bytes < AMPH_PAGED_WS_BYTES)
     return api_fail(AMPH_ERR_WORKSPACE, "scratch: %u bytes needed, 256-byte aligned", AMPH_PAGED_WS_BYTES);
@@ -1003,7 +1004,7 @@ amph_status amph_paged_attention(const amph_paged_cache* cache, const void* q, i
   p.page_shift = shift; p.n_pages = cache->n_pages;
   const int64_t cap = (int64_t)table_stride << shift;
   p.cap = cap > 0x7fff0000 ? 0x7fff0000 : (int)cap;
-  p.scale_log2 = (scale == 0.f ? 1.0f / sqrtf((float)cache->head_dim) : scale) * kLog2e;
+  p.scale_log2 = scale_log2;
   cudaStream_t st = (cudaStream_t)stream;
   if (!ws_clean) {
     const cudaError_t e = cudaMemsetAsync(ws_dev, 0, AMPH_PAGED_WS_COUNTERS, st);

@@ -16,6 +16,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <limits>
 #include <map>
 #include <optional>
 #include <unordered_map>
@@ -251,6 +252,8 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor *q = tensor(a[1]), *table = tensor(a[2]), *lens = tensor(a[3]), *out_in = tensor(a[5]), *lse = tensor(a[6]), *status = tensor(a[7]);
   const double scale = PyFloat_AsDouble(a[4]);
   if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+  float scale_f = (float)scale;                          // 0 means 1 / sqrt(head_dim): not what a scale too small for fp32 asks for
+  if (scale_f == 0.f && scale != 0.0) scale_f = std::numeric_limits<float>::denorm_min();
   if (!on(q, dev, type) || q->dim() != 3 || !q->is_contiguous() || q->size(2) != c->c.head_dim || q->size(0) > 0x7fffffff || q->size(1) > 0x7fffffff)
     return not_these();
   const int64_t seqs = q->size(0), heads = q->size(1);
@@ -265,7 +268,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const cudaStream_t stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
   Scratch& ws = attention_scratch(dev, stream);
   const int rc = lib.paged_attention(&c->c, q->data_ptr(), (int)heads, (const int32_t*)lens->data_ptr(), (const int32_t*)table->data_ptr(), (int)seqs,
-                                     (int)table->size(1), (float)scale, out.data_ptr(), lse ? (float*)lse->data_ptr() : nullptr, ws.t.data_ptr(),
+                                     (int)table->size(1), scale_f, out.data_ptr(), lse ? (float*)lse->data_ptr() : nullptr, ws.t.data_ptr(),
                                      AMPH_PAGED_WS_BYTES, ws.clean, status ? (int32_t*)status->data_ptr() : nullptr, stream);
   ws.clean = rc == AMPH_OK;
   return give(out, rc);

@@ -163,6 +163,21 @@ def test_attention_of_many_sequences(dtype):
     _check_attention(out, lse, q, kp, vp, table, lens, scale=0.3)
 
 
+@pytest.mark.parametrize("scale", [1e-50, -1e-50, 1e-300, 1e-40])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_scales_too_small_to_matter(dtype, scale):
+    """Every key has the same weight; 0 in fp32, which stands for 1 / sqrt(head_dim), is not what such a scale becomes."""
+    from paper_2406_13170_b200 import PagedCache, paged_attention
+    g = _gen(19)
+    lens = [1, 100, 0, 700]
+    table, n_pages = _table(lens, 16, g)
+    kp, vp = _normal(g, n_pages, 2, 16, 128, dtype=dtype), _normal(g, n_pages, 2, 16, 128, dtype=dtype)
+    q = _normal(g, len(lens), 4, 128, dtype=dtype)
+    lse = torch.empty(len(lens), 4, device=DEV)
+    out = paged_attention(PagedCache(kp, vp), q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), scale=scale, lse=lse)
+    _check_attention(out, lse, q, kp, vp, table, lens, scale=scale)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("page", [1, 8, 16, 64])
 def test_slots_behind_a_sequence_are_not_looked_at(dtype, page):

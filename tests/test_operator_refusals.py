@@ -72,6 +72,12 @@ def test_attention_refuses_an_output_that_overlaps_its_queries(L, n_seqs, dtype,
         assert _attend(L, _cache(dtype=dtype), q=far, out=out, n_seqs=n_seqs, ws=None) == 5       # (refused for another reason: no launch)
 
 
+@pytest.mark.parametrize("scale", [2.5e38, -2.5e38, 3.4e38])
+def test_attention_refuses_scales_that_overflow_in_the_kernel(L, scale):
+    """Scores are taken in units of log 2: the scale times log2(e) has to be a number too (an infinite one makes every score of 0 NaN)."""
+    assert _attend(L, scale=scale) == 1 and "scale" in _message(L)
+
+
 def test_null_cache_and_empty_batches(L):
     assert L.amph_paged_attention(None, P, 8, P, P, 3, 4, 0.0, 2 * P, None, P, b.AMPH_PAGED_WS_BYTES, 0, None, None) == 1
     assert _attend(L, n_seqs=0) == 0                  # nothing to do: no launch
