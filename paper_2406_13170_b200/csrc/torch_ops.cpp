@@ -177,6 +177,7 @@ PyObject* project_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
       (a[8] != Py_None && (!on(status, ad->device, at::kInt) || !status->is_contiguous() || status->numel() < 1)))
     return not_these();
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)ad->device);
+  if (rows == 0) return give(y_in ? *y_in : make({0, ld}, y_type, ad->device), AMPH_OK);
   size_t need = 0;
   if (const auto known = ad->bytes.find((int)rows); known != ad->bytes.end()) {
     need = known->second;

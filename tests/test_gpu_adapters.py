@@ -246,6 +246,25 @@ def test_an_output_as_the_next_call_s_weights():
         x = x.roll(1, 0)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_an_empty_batch(dtype):
+    """Answered as the paged operators answer it: nothing is launched."""
+    from paper_2406_13170_b200 import Adapters, AmphError, project_adapters
+    z = lambda *s, dt=dtype: torch.zeros(s, dtype=dt, device=DEV)                 # noqa: E731
+    ad, w, none = Adapters(z(2, 3, 8, 128), z(2, 3, 256, 8)), [z(256, 128)] * 3, z(0, dt=torch.int32)
+    tc = dtype is torch.bfloat16
+    for x in (z(16, 128), z(0, 128)):
+        y = project_adapters(x, w, 0, tc, ad, none)
+        assert y.shape == (0, 768) and y.dtype is dtype and y.is_cuda
+        assert project_adapters(x, w, 0, tc, ad, none, y_dtype=torch.float32).dtype is torch.float32
+        y = z(0, 768)
+        assert project_adapters(x, w, 0, tc, ad, none, y=y) is y
+    for bad in (lambda: project_adapters(z(16, 128), w[:2], 0, tc, ad, none), lambda: project_adapters(z(16, 128), w, 0, tc, ad, z(1, dt=torch.int32)),
+                lambda: project_adapters(z(16, 128), w, 0, tc, ad, none, y=z(1, 768))):
+        with pytest.raises(AmphError):
+            bad()
+
+
 def test_python_refusals():
     from paper_2406_13170_b200 import Adapters, AmphError, project_adapters
     z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device=DEV)        # noqa: E731
