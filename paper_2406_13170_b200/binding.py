@@ -519,6 +519,8 @@ def project_adapters(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use
     """amph_project_adapters: y[r] = x[r] . W^T + scale (x[r] . a^T) . b^T with the adapter row_adapter[r] (int32 [rows], < 0: none).
 
     x, ws, rows (or 0: an empty batch), use_tensor_core as for `project`; y [rows, n_seg * out] of y_dtype (default: x's type)."""
+    if type(ws) is not list:
+        ws = tuple(ws)
     r = (_torch_ops or _ops()).project_adapters(adapters.handle, x, ws, rows, use_tensor_core, row_adapter, y, y_dtype, status)
     if type(r) is int or r is NotImplemented:
         if r is NotImplemented:

@@ -265,6 +265,27 @@ def test_an_empty_batch(dtype):
             bad()
 
 
+def test_any_sequence_of_weights():
+    """As for `project`: a tuple, a module's list of parameters, what indexes and counts itself."""
+    from paper_2406_13170_b200 import Adapters, project, project_adapters
+    c = _ints(torch.Generator(device=DEV).manual_seed(10), -1, 1, 16 + 2 * 256, 128, dtype=torch.bfloat16)
+    x, w = c[:16], [c[16: 272], c[272:]]
+    ad = Adapters(torch.zeros(2, 2, 8, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(2, 2, 256, 8, dtype=torch.bfloat16, device=DEV))
+    at = torch.zeros(5, dtype=torch.int32, device=DEV)
+
+    class Two:
+        def __len__(self):
+            return 2
+
+        def __getitem__(self, i):
+            return w[i]
+
+    want = project_adapters(x, w, 5, True, ad, at, y_dtype=torch.float32)
+    for ws in (tuple(w), torch.nn.ParameterList([torch.nn.Parameter(t, requires_grad=False) for t in w]), Two()):
+        assert torch.equal(project(x, ws, 5, True), want)
+        assert torch.equal(project_adapters(x, ws, 5, True, ad, at, y_dtype=torch.float32), want)
+
+
 def test_python_refusals():
     from paper_2406_13170_b200 import Adapters, AmphError, project_adapters
     z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device=DEV)        # noqa: E731
