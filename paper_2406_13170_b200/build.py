@@ -1,4 +1,7 @@
-"""Builds libamph.so (the C-ABI library) in-tree with nvcc for sm_100a, and torch_ops.so (torch tensors to its operators) beside it."""
+"""Builds libamph.so (the C-ABI library) in-tree with nvcc for sm_100a, and torch_ops.so (torch tensors to its operators) beside it.
+
+The library needs nvcc alone: `python paper_2406_13170_b200/build.py --library` (or build(ops=False)) leaves out torch_ops.so, which needs
+torch's and Python's headers."""
 from __future__ import annotations
 
 import os
@@ -14,33 +17,42 @@ LIB = os.path.join(HERE, "libamph.so")
 OPS = os.path.join(HERE, "torch_ops.so")
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(OPS):
+def _stale(target: str) -> bool:
+    if not os.path.exists(target):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(OPS))
+    t = os.path.getmtime(target)
     deps = [os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc"))]
     deps.append(os.path.join(ROOT, "include", "amph.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
-        return LIB
+def build(force: bool = False, verbose: bool = False, ops: bool = True) -> str:
+    """Builds what is missing or older than its sources; a fault of torch_ops.so is raised once the library is there."""
+    make_lib, make_ops = force or _stale(LIB), ops and (force or _stale(OPS))
+    running = fault = None
+    if make_ops:
+        try:
+            running = subprocess.Popen(_ops_command())
+        except (OSError, ImportError) as e:
+            fault = e
+    try:
+        if make_lib:
+            subprocess.run(_library_command(verbose), check=True)
+    finally:
+        rc = running.wait() if running else 0
+    if fault or rc:
+        raise RuntimeError(f"torch_ops.so was not built ({fault or f'the compiler returned {rc}'}); libamph.so is there") from fault
+    return LIB
+
+
+def _library_command(verbose: bool) -> list:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
            "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
            "-I", os.path.join(HERE, "csrc")]
     if verbose:
         cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(HERE, "csrc", s) for s in SOURCES] + ["-o", LIB, "-lcudart"]
-    ops = subprocess.Popen(_ops_command())
-    try:
-        subprocess.run(cmd, check=True)
-    finally:
-        rc = ops.wait()
-    if rc:
-        raise subprocess.CalledProcessError(rc, ops.args)
-    return LIB
+    return cmd + [os.path.join(HERE, "csrc", s) for s in SOURCES] + ["-o", LIB, "-lcudart"]
 
 
 def _ops_command() -> list:
@@ -55,4 +67,4 @@ def _ops_command() -> list:
 
 
 if __name__ == "__main__":
-    print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build(force="--force" in sys.argv, verbose="-v" in sys.argv, ops="--library" not in sys.argv))
