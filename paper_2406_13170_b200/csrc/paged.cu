@@ -7,6 +7,7 @@
 #include <new>
 
 #include "amph_internal.cuh"
+#include "line.cuh"
 
 namespace amph {
 namespace {
@@ -570,18 +571,6 @@ __device__ __noinline__ Sums add_parts(const float* all, size_t stride, int ahea
       if (c + q * step < count) add_scaled(a, weight(ml[q].x, m), o[q], ml[q].y);
   }
   return a;
-}
-
-// a * b / d, of which the product mostly has 32 bits (a 64-bit division is about 100 instructions)
-__device__ __forceinline__ long long mul_div(long long a, int b, long long d) {
-  const unsigned long long x = (unsigned long long)a * (unsigned)b;
-  return ((x | (unsigned long long)d) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)d) : (long long)(x / (unsigned long long)d);
-}
-
-// The block that holds unit u when `total` units are spread over n blocks (block c begins at total * c / n).
-__device__ __forceinline__ int block_of(long long u, long long total, int n) {
-  const unsigned long long x = (unsigned long long)(u + 1) * (unsigned)n - 1;
-  return (int)(((x | (unsigned long long)total) >> 32) == 0 ? (uint32_t)x / (uint32_t)total : x / (unsigned long long)total);
 }
 
 // Columns 4 i .. 4 i + 3 of an item from a block's warps
