@@ -375,8 +375,9 @@ typedef struct {
  * values' way into the pages.  Row r belongs to sequence row_seq[r] and sits at position row_pos[r] (device int32 [rows]); a
  * row with row_seq[r] < 0 is skipped, nothing is written for it; one whose sequence, position or page does not exist is skipped and
  * status_dev is set.  q, k, v: src_dtype [rows][n_heads or n_kv_heads][head_dim], rows q_stride / k_stride / v_stride
- * ELEMENTS apart (slices of a projection's output), 16-byte aligned; AMPH_DTYPE_F32, or AMPH_DTYPE_BF16.  q_out: [rows][n_heads][head_dim] of the cache's dtype.  q = q_out = NULL
- * with n_heads = 0: keys and values only.  Rows of one call must not name the same slot (which of them is kept is unspecified). */
+ * ELEMENTS apart (slices of a projection's output), 16-byte aligned; AMPH_DTYPE_F32, or AMPH_DTYPE_BF16.  q_out: [rows][n_heads][head_dim] of the cache's dtype;
+ * it may be q itself where that is of the cache's dtype with q_stride = n_heads * head_dim (or one row), and must not overlap q in any other way,
+ * nor k and v; the pages must not overlap any of them.  q = q_out = NULL with n_heads = 0: keys and values only.  Rows of one call must not name the same slot (which of them is kept is unspecified). */
 amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                              const void* v, int64_t v_stride, int32_t src_dtype, int32_t n_heads, int32_t rows,
                              const int32_t* row_seq, const int32_t* row_pos, const int32_t* table, int32_t n_seqs,

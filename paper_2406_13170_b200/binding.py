@@ -595,7 +595,8 @@ def paged_write(cache: PagedCache, q: Optional[torch.Tensor], k: torch.Tensor, v
     """amph_paged_write: rotates q and k of every row by its position, puts k and v into the pages, returns q.
 
     q [rows, n_heads * head_dim] (or None), k, v [rows, n_kv_heads * head_dim], fp32 or bf16 (one type), each row contiguous (slices
-    of a projection's output); row_seq, row_pos int32 [rows], row_seq < 0: the row is skipped (its place in a new q_out is not set)."""
+    of a projection's output); row_seq, row_pos int32 [rows], row_seq < 0: the row is skipped (its place in a new q_out is not set).
+    q_out may be q (of the cache's type, contiguous); any other overlap of outputs and inputs is a fault.  theta is taken in fp32."""
     r = (_torch_ops or _ops()).paged_write(cache.handle, q, k, v, row_seq, row_pos, table, theta, q_out, status)
     if type(r) is int or r is NotImplemented:
         if r is NotImplemented:

@@ -20,7 +20,7 @@ template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T* p) {
   Raw8<T> r;
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = reinterpret_cast<const uint4*>(p)[i];
   return r;
 }
 __device__ __forceinline__ void values(const Raw8<float>& r, float (&v)[8]) {
@@ -81,7 +81,7 @@ __device__ __forceinline__ float2 cos_sin_of_phase(u64 phase) {
 }
 
 // Grid (row, part of the row's heads); an item is eight rotation pairs of one head (eight values twice for v), a thread has ITEMS, whose
-// loads are under way while the row's place in the cache is looked up.  Bound: HBM for many rows, latency for few (see run_write).
+// loads are under way while the row's place in the cache is looked up.  A thread writes what it has read and nobody else reads, so q_out may be q.  Bound: HBM for many rows, latency for few (see run_write).
 template <typename TS, typename TD, int ITEMS>
 __global__ void __launch_bounds__(kWriteThreads) paged_write_kernel(const __grid_constant__ WriteParams p) {
   pdl_wait();

@@ -235,6 +235,25 @@ def test_infinite_and_nan_scores():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("wide", [False, True], ids=["narrow", "wide"])
+def test_infinite_values(dtype, wide):
+    """An infinity among a sequence's own values makes its column infinite or NaN in the heads that read it, and changes nothing else."""
+    from paper_2406_13170_b200 import PagedCache, paged_attention
+    g = _gen(16)
+    lens = [40, 100, 700]
+    table, n_pages = _table(lens, 16, g, width=9000 if wide else None)
+    kp, vp = _normal(g, n_pages, 2, 16, 64, dtype=dtype), _normal(g, n_pages, 2, 16, 64, dtype=dtype)
+    q, n = _normal(g, 3, 8, 64, dtype=dtype), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    good = paged_attention(PagedCache(kp, vp), q, table, n)
+    vp[int(table[1, 5]), 1, 9, 33] = math.inf
+    vp[int(table[2, 40]), 0, 2, 7] = -math.inf
+    out = paged_attention(PagedCache(kp, vp), q, table, n)
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[1, 4:, 33] = hit[2, :4, 7] = True
+    assert not torch.isfinite(out[hit]).any() and torch.equal(out[~hit], good[~hit])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("page", [4, 16])
 def test_pages_and_lengths_that_do_not_exist(dtype, page):
     """They are reported, count as absent, and the other sequences' rows are what they are without them."""
@@ -373,6 +392,24 @@ def test_write(heads, kv, dh, page, seqs, source, dtype, theta):
 ])
 def test_write_of_many_rows(heads, kv, dh, page, seqs, source, dtype):
     test_write(heads, kv, dh, page, seqs, source, dtype, 10000.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv,dh,rows", [(32, 8, 128, 1), (5, 1, 64, 7), (40, 40, 128, 64), (32, 8, 128, 900)])
+def test_queries_rotated_in_place(heads, kv, dh, rows, dtype):
+    from paper_2406_13170_b200 import PagedCache, paged_write
+    g = _gen(rows)
+    table, n_pages = _table([rows + 40], 16, g)
+    kp, vp = (torch.zeros(n_pages, kv, 16, dh, dtype=dtype, device=DEV) for _ in range(2))
+    q, k, v = _normal(g, rows, heads, dh, dtype=dtype), _normal(g, rows, kv, dh, dtype=dtype), _normal(g, rows, kv, dh, dtype=dtype)
+    seq = torch.where(torch.arange(rows, device=DEV) % 5 == 3, -1, 0).to(torch.int32)
+    pos = torch.arange(40, 40 + rows, dtype=torch.int32, device=DEV)
+    before = q.clone()
+    want = paged_write(PagedCache(kp, vp), q, k, v, seq, pos, table, q_out=before.clone())
+    keys = kp.clone()
+    kp.zero_()
+    assert paged_write(PagedCache(kp, vp), q, k, v, seq, pos, table, q_out=q) is q
+    assert torch.equal(q, want) and torch.equal(kp, keys) and torch.equal(q[seq < 0], before[seq < 0])
 
 
 def test_angles_of_far_positions():
