@@ -352,7 +352,8 @@ typedef struct {
  * x, w, n_seg, out, in, rows (1..512), x_rows_cap, dtype and use_tensor_core as for amph_project (small bf16 projections, and those with
  * use_tensor_core = 0, run on the warp-level tensor cores).  y: [rows][n_seg*out] of
  * y_dtype, 16-byte aligned (AMPH_DTYPE_F32, or AMPH_DTYPE_BF16 with bf16 weights: the sums, held in fp32, are rounded once).
- * y must not overlap an input.
+ * With bf16 weights the low-rank products sum_k x a, held in fp32 and times scale, enter the second sum in two bf16 halves: up to 2^-17 of
+ * them is lost, in an fp32 y too, and where an element of b is infinite y can be NaN in place of an infinity.  y must not overlap an input.
  * ws_dev: device scratch, 256-byte aligned, at least amph_project_adapters_bytes() bytes; nothing in it needs to be set and nothing
  * is kept in it.  Calls that may overlap on the GPU need scratch of their own.  Make the first call on a device outside a stream capture. */
 amph_status amph_project_adapters_bytes(int32_t n_seg, int32_t out, int32_t rows, int32_t rank, size_t* ws_bytes);
@@ -375,7 +376,7 @@ typedef struct {
  * values' way into the pages.  Row r belongs to sequence row_seq[r] and sits at position row_pos[r] (device int32 [rows]); a
  * row with row_seq[r] < 0 is skipped, nothing is written for it; one whose sequence, position or page does not exist is skipped and
  * status_dev is set.  q, k, v: src_dtype [rows][n_heads or n_kv_heads][head_dim], rows q_stride / k_stride / v_stride
- * ELEMENTS apart (slices of a projection's output), 16-byte aligned; AMPH_DTYPE_F32, or AMPH_DTYPE_BF16.  q_out: [rows][n_heads][head_dim] of the cache's dtype;
+ * ELEMENTS apart (slices of a projection's output), 16-byte aligned; AMPH_DTYPE_F32 or AMPH_DTYPE_BF16.  q_out: [rows][n_heads][head_dim] of the cache's dtype;
  * it may be q itself where that is of the cache's dtype with q_stride = n_heads * head_dim (or one row), and must not overlap q in any other way,
  * nor k and v; the pages must not overlap any of them.  q = q_out = NULL with n_heads = 0: keys and values only.  Rows of one call must not name the same slot (which of them is kept is unspecified). */
 amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
