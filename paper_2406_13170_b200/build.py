@@ -33,7 +33,7 @@ def build(force: bool = False, verbose: bool = False, ops: bool = True) -> str:
     if make_ops:
         try:
             running = subprocess.Popen(_ops_command())
-        except (OSError, ImportError) as e:
+        except Exception as e:
             fault = e
     try:
         if make_lib:

@@ -60,8 +60,11 @@ def test_the_library_needs_no_torch_headers(commands, fault):
     assert commands["ran"] == ["torch_ops.so", "libamph.so"]              # the library is not built again
 
 
-def test_without_torch(commands, monkeypatch):
-    monkeypatch.setattr(amph_build, "_ops_command", lambda: (_ for _ in ()).throw(ImportError("torch")))
+@pytest.mark.parametrize("fault", [ImportError("torch"), RuntimeError("torch of another CUDA")], ids=["no_torch", "another_torch"])
+def test_without_torch(commands, monkeypatch, fault):
+    def command():
+        raise fault
+    monkeypatch.setattr(amph_build, "_ops_command", command)
     with pytest.raises(RuntimeError, match="torch"):
         amph_build.build()
     assert os.path.exists(amph_build.LIB)

@@ -47,7 +47,7 @@ def _ran(call):
 @pytest.fixture(scope="module")
 def kernels():
     """Kernels of a call of each path.  In a process of its own: a test that counts a replayed graph's kernels was given too few of them behind a
-    profiler's runs in the same process (once in two runs of all tests)."""
+    profiler's runs in the same process (seen once, in a run of all tests)."""
     r = subprocess.run([sys.executable, "-m", "tests.test_gpu_adapters_paths"], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
     return json.loads(r.stdout.strip().splitlines()[-1])
