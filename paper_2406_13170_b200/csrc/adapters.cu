@@ -190,7 +190,7 @@ __device__ __forceinline__ void halves(float v, bf16& hi, bf16& lo) {
 // `beside`: the kernel ahead is the tensor-core projection, which starts this one once everything ahead of itself is done, so it takes
 // the SMs and the shared memory that the projection leaves; what it reads is older than the projection (and past L1, see pdl_wait); only the first block
 // waits for the projection, so that both are done when this one is.  (Ahead of the projection, q / k / v of 64 rows of 24
-// tenants took 36.1 us in all, 28.0 now; gate / up of 37 rows at rank 64 48.5, 44.2 now; 512 rows, see down_splits, 59 and 47.9.)  72 registers:
+// tenants took 36.1 us in all, 28.0 now; gate / up of 37 rows at rank 64 48.5, 42.9 now; 512 rows, see down_splits, 59 and 48.7.)  72 registers:
 // beside a CTA of the pair kernel an SM's schedulers have room for two such warps each, not for two of 80.
 // Bound: latency for a few rows, the adapters' bytes for many tenants.
 constexpr int kDownCols = 32;
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdapterArgs 
 
 // adapter_down and adapter_up in one for a few rows (kFewRows) and a small rank: grid (128 columns, tile, segment), a block works out its
 // tile's t itself while the projection ahead still runs (which has started it once everything ahead of itself was done, see pdl_wait), holds b in registers,
-// waits, and adds the partial sums.  Its warps share K for t and have 16 columns each for y.  (One row of 4096 x 4096, rank 16: 9.3 us, 11.3
+// waits, and adds the partial sums.  Its warps share K for t and have 16 columns each for y.  (One row of 4096 x 4096, rank 16: 9.4 us, 11.3
 // with the two kernels, and one launch less for the host.)
 constexpr int kFewRows = 16, kFewRank = 32;
 template <int QUADS, typename TY>
@@ -664,7 +664,7 @@ int most_tiles(int rows, int n_adapters) {
   return n < rows ? (int)n : rows;
 }
 // K ranges of adapter_down, a cluster: at most `most` blocks in all, 64 columns of k for each warp at least.  444: three blocks per SM; 168
-// beside the pair kernel, which leaves room for one block on each SM that it uses (512 rows, out 4096, in 11008, rank 32: 47.9 us, 52.9 with 444;
+// beside the pair kernel, which leaves room for one block on each SM that it uses (512 rows, out 4096, in 11008, rank 32: 48.7 us, 52.9 with 444;
 // 128 rows, three matrices of 5120 x 5120, rank 16, 32 adapters: 43.7 us, 54.3 with 148 and so no cluster).
 int down_splits(int in, int blocks, int most) {
   int s = 1;
