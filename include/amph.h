@@ -389,7 +389,7 @@ amph_status amph_paged_write(const amph_paged_cache* cache, const void* q, int64
  * lens: device int32 [n_seqs] (the new token included, so amph_paged_write comes first); 0: out[s] = 0.  A length outside
  * 0 .. table_stride * page_size is clamped and status_dev is set; the keys of a page that does not exist count as absent, and status_dev is set.
  * q, out: [n_seqs][n_heads][head_dim] of the cache's dtype, 16-byte aligned; out must not overlap q.  lse: float [n_seqs][n_heads], natural logarithm of
- * sum_p w_p (-inf without keys), or NULL.  scale: 0 means 1 / sqrt(head_dim).  n_heads: a multiple of n_kv_heads, at most 1024;
+ * sum_p w_p (-inf without keys), or NULL.  scale: 0 means 1 / sqrt(head_dim); finite, also times log2(e).  n_heads: a multiple of n_kv_heads, at most 1024;
  * n_seqs at most AMPH_PAGED_MAX_SEQS.  ws_dev: device scratch of AMPH_PAGED_WS_BYTES, 256-byte aligned, for the parts of sequences that several
  * blocks share.  Its first AMPH_PAGED_WS_COUNTERS bytes must be zero when the kernel starts, and every call leaves them zero: with
  * ws_clean = 0 the call clears them itself (scratch with any contents), with ws_clean = 1 the caller vouches for them (cleared

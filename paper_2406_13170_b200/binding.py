@@ -413,7 +413,8 @@ def project_noalloc(x: torch.Tensor, ws: Sequence[torch.Tensor], rows: int, use_
 # ---------------------------------------------------------------------------------------------------------------------
 # Operators for decoding many requests over one set of weights.  They run on torch's current stream of the tensors' device, never
 # synchronise, and return tensors whose contents are there in stream order.  paged_attention keeps 5 MB of scratch per stream that it is called
-# on (csrc/torch_ops.cpp), the others none.
+# on (csrc/torch_ops.cpp), the others none.  They may be captured with torch.cuda.graph (scratch comes from torch's allocator, which has to know
+# of the capture); a capture made another way calls the library with scratch of its own.
 # ---------------------------------------------------------------------------------------------------------------------
 _DTYPES = {torch.float32: AMPH_DTYPE_F32, torch.bfloat16: AMPH_DTYPE_BF16}
 
